@@ -352,6 +352,124 @@ int fem_gla_fwd(const void* Q, const void* K, const void* V, const float* G,
                 int B, int H, int T, int d_k, int d_v, int chunk,
                 int dtype, void* ws, size_t ws_bytes, hipStream_t stream);
 
+/* ---- the paged key/value cache and the read over it ------------------------
+ *
+ * A cache is two pools of pages, each page holding `page` consecutive tokens of
+ * one sequence for every cached head: K [pages, heads, page, d_qk] and V
+ * [pages, heads, page, d_v].  A sequence's tokens lie in the pages that its row
+ * of the table names, in order; a page may serve several sequences (a shared
+ * prefix).
+ */
+typedef enum {
+  FEM_KV_BF16 = 0,  /* bfloat16 values                                        */
+  FEM_KV_E4M3 = 1,  /* 8-bit codes with a scale for every 32 channels: OCP     */
+  FEM_KV_INT8 = 2   /*   float8 e4m3, or signed integers                       */
+} fem_kv_type;
+
+/*
+ * Quantised rows: channels 32 c .. 32 c + 31 of a row share the scale 2^e,
+ * stored as the byte e + 127 in k_scale [pages, heads, page, d_qk / 32] and
+ * v_scale [.., d_v / 32].  e is the smallest integer, at least -100, with
+ * max |x| <= M 2^e, M = 448 (e4m3) or 127 (int8); a code is x 2^-e rounded to
+ * nearest even, so none saturates.  The value code 2^e is exactly a bf16 number:
+ * a read over a quantised cache is the bf16 read over its values.  A block with
+ * an inf or NaN gets the byte 255 and reads as NaN.
+ */
+typedef struct {
+  void* k;                /* 16-byte aligned                                   */
+  void* v;
+  unsigned char* k_scale; /* NULL for FEM_KV_BF16                              */
+  unsigned char* v_scale;
+  int pages;              /* >= 1                                              */
+  int page;               /* tokens of a page: a power of two, 16 .. 1024      */
+  int heads;              /* cached heads                                      */
+  int d_qk, d_v;          /* pairs as fem_softmax_fwd_ex                       */
+  int type;               /* fem_kv_type                                       */
+} fem_paged_cache;
+
+/*
+ * The sequences of a call.  Sequence b has the new tokens q_start[b] ..
+ * q_start[b+1] - 1 of the packed tensors (none is fine), and lens[b] tokens in
+ * the cache, the new ones included: new token i has position lens[b] - n_b + i.
+ * Rows of the packed tensors behind q_start[n_seq] belong to no sequence.
+ *
+ * The arrays are DEVICE memory and are not read on the host.  A sequence whose
+ * numbers contradict each other (q_start not ascending within 0 .. n_tok, more
+ * new tokens than max_q or, for an append or a causal read, than lens[b], a
+ * length past table_len * page), or one of whose pages in use lies outside the
+ * pool, reads as NaN (an append skips what has no slot); nothing outside the
+ * buffers is touched.  Starts that are not ascending leave it open which tokens
+ * are read or stored.
+ */
+typedef struct {
+  const int* q_start;     /* [n_seq + 1]                                       */
+  const int* lens;        /* [n_seq]                                           */
+  const int* table;       /* [n_seq, table_len] page numbers; entries past a
+                             sequence's last page are not read                 */
+  int n_seq, table_len;   /* n_seq <= 65535, table_len * page <= 2^30          */
+  int n_tok;              /* rows of the packed tensors                        */
+  int max_q;              /* no sequence has more new tokens                   */
+} fem_paged_batch;
+
+/*
+ * Stores the new tokens' keys and values.
+ *
+ *   k : [n_tok, heads, d_qk] bfloat16, token t at k + t * k_ld elements
+ *   v : [n_tok, heads, d_v] bfloat16, token t at v + t * v_ld
+ *       (k_ld, v_ld multiples of 8: slices of one projection's output will do)
+ *
+ * Two new tokens must not share a slot (two sequences that share the page they
+ * write to): what such a slot then holds is unspecified.  Returns a fem_status.
+ */
+int fem_cache_append(const fem_paged_cache* cache, const fem_paged_batch* batch,
+                     const void* k, long long k_ld, const void* v, long long v_ld,
+                     hipStream_t stream);
+
+/*
+ * Reads the cache back: rows 0 .. min(lens[b], L) - 1 of sequence b as bfloat16
+ * (exact) into k [n_seq, heads, L, d_qk] and v [n_seq, heads, L, d_v], the layout
+ * of the dense reads; either may be NULL.  Later rows are left as they were.  A
+ * row whose page lies outside the pool reads as NaN; a sequence with a length
+ * outside [0, table_len * page] is left as it was.  q_start, n_tok and max_q are
+ * not used.  Returns a fem_status.
+ */
+int fem_cache_gather(const fem_paged_cache* cache, const fem_paged_batch* batch,
+                     void* k, void* v, int L, hipStream_t stream);
+
+/*
+ * The softmax-prior read of new tokens over a paged cache: token i of sequence b
+ * reads the cached tokens 0 .. lens[b] - n_b + i (its own position included; a
+ * chunk of a prompt, drafted tokens or, with one token, a decoding step), or with
+ * FEM_FLAG_ENCODER all lens[b] of them (an encoder's states, whose number has
+ * nothing to do with the new tokens'):
+ *
+ *   out[t,h,j] = (1/beta[g,j]) log sum_i p(i) exp(beta[g,j] v[g,i,j]),
+ *   p = softmax_i( q[t,h] . k[g,i] / sqrt(d_qk) ),   g = h / (H / heads)
+ *
+ *   q     : [n_tok, H, d_qk] bfloat16, token t at q + t * q_ld elements (q_ld a
+ *           multiple of 8); H a multiple of the cached heads, H / heads query
+ *           heads sharing one
+ *   beta  : [heads, d_v] float32, > 0: a temperature for every cached channel
+ *   out   : [n_tok, H, d_v] float32, or bfloat16 with FEM_FLAG_OUT_BF16.  Rows of
+ *           no sequence are left as they were; a token that sees no key (lens[b] =
+ *           0 with FEM_FLAG_ENCODER) reads NaN.
+ *   flags : an OR of fem_flags
+ *
+ * Cached rows at or past lens[b] may hold anything.  The same inputs give the same
+ * bits.  Probabilities enter the product as bf16, exponentials of channels with
+ * beta < 0.5 as bf16 hi + lo parts, of the others as bf16 (2^-8 / beta of the
+ * read at most); sums are float32.
+ *
+ * fem_paged_workspace_bytes gives the scratch that these sizes need (0 for
+ * arguments outside the supported set); it depends on the sizes in the two
+ * structs and H alone, not on the device arrays.  Returns a fem_status.
+ */
+size_t fem_paged_workspace_bytes(const fem_paged_cache* cache, const fem_paged_batch* batch, int H);
+
+int fem_paged_fwd(const fem_paged_cache* cache, const fem_paged_batch* batch,
+                  const void* q, long long q_ld, const float* beta, void* out,
+                  int H, int flags, void* ws, size_t ws_bytes, hipStream_t stream);
+
 /* Static, NUL-terminated name of a status code (never NULL). */
 const char* fem_status_str(int status);
 

@@ -27,3 +27,4 @@ from .fem_oracle import (  # noqa: F401
     gla_features,
     posterior,
 )
+from .paged import codes_of, fem_paged, stored, values_of  # noqa: F401

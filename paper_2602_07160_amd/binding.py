@@ -22,10 +22,26 @@ FEM_DTYPE = {torch.float32: 0, torch.bfloat16: 1}
 EXPORTS = ("fem_softmax_fwd", "fem_softmax_fwd_ex", "fem_softmax_fwd_train", "fem_softmax_bwd",
            "fem_softmax_bwd_workspace_bytes", "fem_softmax_gated_fwd", "fem_softmax_decode",
            "fem_softmax_decode_workspace_bytes", "fem_softmax_decode_noalloc", "fem_linear_fwd", "fem_linear_workspace_bytes",
-           "fem_gla_fwd", "fem_gla_workspace_bytes", "fem_status_str")
+           "fem_gla_fwd", "fem_gla_workspace_bytes", "fem_cache_append", "fem_cache_gather",
+           "fem_paged_workspace_bytes", "fem_paged_fwd", "fem_status_str")
 
 FEM_FLAG_ENCODER = 1
 FEM_FLAG_OUT_BF16 = 2
+
+# fem_kv_type of a pool's element type
+FEM_KV = {torch.bfloat16: 0, torch.float8_e4m3fn: 1, torch.int8: 2}
+
+
+class _Cache(ctypes.Structure):  # fem_paged_cache
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p),
+                ("v_scale", ctypes.c_void_p)] + [
+                    (n, ctypes.c_int) for n in ("pages", "page", "heads", "d_qk", "d_v", "type")]
+
+
+class _Batch(ctypes.Structure):  # fem_paged_batch
+    _fields_ = [("q_start", ctypes.c_void_p), ("lens", ctypes.c_void_p),
+                ("table", ctypes.c_void_p)] + [
+                    (n, ctypes.c_int) for n in ("n_seq", "table_len", "n_tok", "max_q")]
 
 _lib = None
 
@@ -71,6 +87,15 @@ def load() -> ctypes.CDLL:
         lib.fem_softmax_bwd.restype = i
         lib.fem_softmax_bwd_workspace_bytes.argtypes = [i, i, i, i]
         lib.fem_softmax_bwd_workspace_bytes.restype = sz
+        cp, bp, ll = ctypes.POINTER(_Cache), ctypes.POINTER(_Batch), ctypes.c_longlong
+        lib.fem_cache_append.argtypes = [cp, bp, vp, ll, vp, ll, vp]
+        lib.fem_cache_append.restype = i
+        lib.fem_cache_gather.argtypes = [cp, bp, vp, vp, i, vp]
+        lib.fem_cache_gather.restype = i
+        lib.fem_paged_workspace_bytes.argtypes = [cp, bp, i]
+        lib.fem_paged_workspace_bytes.restype = sz
+        lib.fem_paged_fwd.argtypes = [cp, bp, vp, ll, f, vp, i, i, vp, sz, vp]
+        lib.fem_paged_fwd.restype = i
         lib.fem_status_str.argtypes = [i]
         lib.fem_status_str.restype = ctypes.c_char_p
         _lib = lib
@@ -420,6 +445,186 @@ def fem_softmax_bwd(q, k, v, beta, out, lse, dout, ws=None, stream=None):
                                  FEM_DTYPE[q.dtype], wsp, wsn, _stream_handle(q.device, stream))
     _check(rc)
     return dq, dk, dv, db
+
+
+class PagedCache:
+    """A paged key/value cache over the caller's pools: k [pages, heads, page,
+    d_qk] and v [pages, heads, page, d_v], both bfloat16, or both
+    torch.float8_e4m3fn or torch.int8 codes with their scale bytes k_scale, v_scale
+    [.., width / 32] (uint8).  The pools stay the caller's; the object holds
+    them and describes them to the library.  ``PagedCache.empty`` allocates them."""
+
+    def __init__(self, k, v, k_scale=None, v_scale=None):
+        if not isinstance(k, torch.Tensor) or k.dtype not in FEM_KV:
+            raise ValueError("the pools must be bfloat16, float8_e4m3fn or int8 tensors")
+        for name, x in (("k", k), ("v", v)):
+            _dev_tensor(x, name, k.dtype)
+            if x.dim() != 4 or x.shape[:3] != k.shape[:3]:
+                raise ValueError("k must be [pages, heads, page, d_qk] and v [pages, heads, page, d_v]")
+        if k.dtype == torch.bfloat16:
+            if k_scale is not None or v_scale is not None:
+                raise ValueError("a bfloat16 cache has no scales")
+        else:
+            for name, x, pool in (("k_scale", k_scale, k), ("v_scale", v_scale, v)):
+                _dev_tensor(x, name, torch.uint8)
+                if tuple(x.shape) != (*pool.shape[:3], pool.shape[3] // 32):
+                    raise ValueError(f"{name} must be [pages, heads, page, width / 32]")
+        if any(x is not None and x.device != k.device for x in (v, k_scale, v_scale)):
+            raise ValueError("the pools must be on one device")
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.device = k.device
+        pages, self.heads, page, self.d_qk = k.shape
+        self.d_v = v.shape[3]
+        self.c = _Cache(k.data_ptr(), v.data_ptr(), None if k_scale is None else k_scale.data_ptr(),
+                        None if v_scale is None else v_scale.data_ptr(), pages, page, self.heads,
+                        self.d_qk, self.d_v, FEM_KV[k.dtype])
+        self.ref = ctypes.byref(self.c)
+
+    @classmethod
+    def empty(cls, pages, heads, d_qk, d_v=None, page=64, dtype=torch.bfloat16, device="cuda"):
+        """A cache with pools of its own (uninitialised)."""
+        def pool(w, dt):
+            return torch.empty((pages, heads, page, w), device=device, dtype=dt)
+
+        d_v = d_qk if d_v is None else d_v
+        scales = (None, None) if dtype == torch.bfloat16 else (pool(d_qk // 32, torch.uint8),
+                                                               pool(d_v // 32, torch.uint8))
+        return cls(pool(d_qk, dtype), pool(d_v, dtype), *scales)
+
+
+class PagedBatch:
+    """The sequences of a call: q_start [B + 1], lens [B] and table [B, table_len],
+    int32 GPU tensors (read on the GPU at each call, so they may change in place
+    between calls), the packed tensors' rows n_tok and the most new tokens of a
+    sequence max_q (default n_tok).  See fem_paged_batch in fem.h."""
+
+    def __init__(self, q_start, lens, table, n_tok=None, max_q=None):
+        _dev_tensor(lens, "lens", torch.int32)
+        _dev_tensor(table, "table", torch.int32)
+        if lens.dim() != 1 or table.dim() != 2 or table.shape[0] != lens.shape[0]:
+            raise ValueError("lens must be [B] and table [B, table_len]")
+        if q_start is not None:
+            _dev_tensor(q_start, "q_start", torch.int32)
+            if tuple(q_start.shape) != (lens.shape[0] + 1,):
+                raise ValueError("q_start must be [B + 1]")
+        if any(x is not None and x.device != lens.device for x in (q_start, table)):
+            raise ValueError("q_start, lens and table must be on one device")
+        self.q_start, self.lens, self.table = q_start, lens, table
+        self.device = lens.device
+        self.n_tok = 0 if n_tok is None else int(n_tok)
+        self.c = _Batch(None if q_start is None else q_start.data_ptr(), lens.data_ptr(),
+                        table.data_ptr(), lens.shape[0], table.shape[1], self.n_tok,
+                        self.n_tok if max_q is None else int(max_q))
+        self.ref = ctypes.byref(self.c)
+
+
+def _paged(cache, batch):
+    if not isinstance(cache, PagedCache) or not isinstance(batch, PagedBatch):
+        raise ValueError("cache must be a PagedCache and batch a PagedBatch")
+    if cache.device != batch.device:
+        raise ValueError("cache and batch must be on one device")
+
+
+def _packed(x, name, n_tok, heads, width, device):
+    """Row stride of a packed [n_tok, heads, width] bf16 tensor whose tokens may
+    lie apart (a slice of one projection's output)."""
+    if not isinstance(x, torch.Tensor) or not x.is_cuda or x.device != device:
+        raise ValueError(f"{name} must be a GPU tensor on the cache's device")
+    if x.dtype != torch.bfloat16:
+        raise ValueError(f"{name} must be bfloat16, got {x.dtype}")
+    if x.dim() != 3 or x.shape[0] != n_tok or x.shape[2] != width or \
+            (heads is not None and x.shape[1] != heads):
+        raise ValueError(f"{name} must be [n_tok, heads, width] of the batch and the cache")
+    s0, s1, s2 = x.stride()
+    if (s2 != 1 and width > 1) or (s1 != width and x.shape[1] > 1):
+        raise ValueError(f"a token's heads must be contiguous in {name}")
+    return s0 if n_tok > 1 else x.shape[1] * width
+
+
+def fem_cache_append(cache, batch, k, v, stream=None) -> None:
+    """Store the batch's new keys k [n_tok, heads, d_qk] and values v [n_tok,
+    heads, d_v] (bf16; tokens may be strided) in the cache, quantised if its pools
+    are."""
+    lib = load()
+    _paged(cache, batch)
+    kld = _packed(k, "k", batch.n_tok, cache.heads, cache.d_qk, cache.device)
+    vld = _packed(v, "v", batch.n_tok, cache.heads, cache.d_v, cache.device)
+    with _on(cache.device):
+        rc = lib.fem_cache_append(cache.ref, batch.ref, k.data_ptr(), kld, v.data_ptr(), vld,
+                                  _stream_handle(cache.device, stream))
+    _check(rc)
+
+
+def fem_cache_gather(cache, batch, k=None, v=None, L=None, stream=None):
+    """The sequences' cached rows as k [B, heads, L, d_qk] and v [B, heads, L, d_v]
+    bf16, the dense reads' layout; rows at or past a sequence's length are left as
+    they were.  Buffers that are not given are allocated with zeros (L: by default
+    the table's length in tokens).  Returns (k, v)."""
+    lib = load()
+    _paged(cache, batch)
+    B, H = batch.c.n_seq, cache.heads
+    if L is None:
+        given = k if k is not None else v
+        L = batch.c.table_len * cache.c.page if given is None else given.shape[2]
+    s = torch.cuda.current_stream(cache.device) if stream is None else stream
+    out = []
+    for name, x, w in (("k", k, cache.d_qk), ("v", v, cache.d_v)):
+        if x is None:
+            if not isinstance(s, torch.cuda.Stream):
+                s = torch.cuda.ExternalStream(int(s), device=cache.device)
+            with torch.cuda.stream(s):
+                x = torch.zeros((B, H, L, w), device=cache.device, dtype=torch.bfloat16)
+        _dev_tensor(x, name, torch.bfloat16)
+        if tuple(x.shape) != (B, H, L, w) or x.device != cache.device:
+            raise ValueError(f"{name} must be [B, heads, L, width] on the cache's device")
+        out.append(x)
+    with _on(cache.device):
+        rc = lib.fem_cache_gather(cache.ref, batch.ref, out[0].data_ptr(), out[1].data_ptr(), L,
+                                  _stream_handle(cache.device, stream))
+    _check(rc)
+    return out[0], out[1]
+
+
+def fem_paged_workspace_bytes(cache, batch, H) -> int:
+    """Exact workspace size (bytes) of fem_paged_fwd with H query heads."""
+    _paged(cache, batch)
+    return int(load().fem_paged_workspace_bytes(cache.ref, batch.ref, int(H)))
+
+
+def fem_paged_fwd(cache, batch, q, beta, causal: bool = True, out=None, out_dtype=torch.float32,
+                  ws=None, stream=None) -> torch.Tensor:
+    """The read of the batch's new tokens q [n_tok, H, d_qk] (bf16; tokens may be
+    strided) over the cache: every token the keys up to its own position, or with
+    causal=False all of its sequence's.  beta: [heads, d_v] fp32.  H / heads query
+    heads share a cached head.  ws: optional uint8 GPU workspace of at least
+    fem_paged_workspace_bytes(...) bytes.  Returns [n_tok, H, d_v], fp32 or bf16
+    (out's type, or out_dtype)."""
+    lib = load()
+    _paged(cache, batch)
+    qld = _packed(q, "q", batch.n_tok, None, cache.d_qk, cache.device)
+    H = q.shape[1]
+    _dev_tensor(beta, "beta", torch.float32)
+    if tuple(beta.shape) != (cache.heads, cache.d_v) or beta.device != cache.device:
+        raise ValueError("beta must be [heads, d_v] on the cache's device")
+    if out is not None:
+        out_dtype = out.dtype
+    if out_dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError("out_dtype must be float32 or bfloat16")
+    if out is None:
+        out = torch.empty((batch.n_tok, H, cache.d_v), device=cache.device, dtype=out_dtype)
+    _dev_tensor(out, "out", out_dtype)
+    if tuple(out.shape) != (batch.n_tok, H, cache.d_v) or out.device != cache.device:
+        raise ValueError("out must be [n_tok, H, d_v] on the cache's device")
+    flags = (0 if causal else FEM_FLAG_ENCODER) | \
+        (FEM_FLAG_OUT_BF16 if out_dtype == torch.bfloat16 else 0)
+    need = 0 if ws is not None else lib.fem_paged_workspace_bytes(cache.ref, batch.ref, H)
+    with _on(cache.device):
+        wst, wsp, wsn = _workspace(need, cache.device, ws, stream)
+        rc = lib.fem_paged_fwd(cache.ref, batch.ref, q.data_ptr(), qld, beta.data_ptr(),
+                               out.data_ptr(), H, flags, wsp, wsn,
+                               _stream_handle(cache.device, stream))
+    _check(rc)
+    return out
 
 
 def workspace_bytes(entry: str, *sizes) -> int:

@@ -2,6 +2,7 @@
 
 #include "fem.h"
 #include "fem_internal.h"
+#include "fem_paged.h"
 
 #include <stdint.h>
 
@@ -48,6 +49,54 @@ bool bwd_args_ok(int B, int H, int T, int d) {
   return sizes_ok(B, H, T, d) && (unsigned long long)H <= 65535ull &&
          (d == 32 || d == 64 || d == 128);
 }
+
+// The cache and the sequences of a paged call: FEM_OK and the kernels' view of
+// them, or what is wrong.  `tokens`: the call has new tokens.
+int paged_args(const fem_paged_cache* c, const fem_paged_batch* s, bool tokens, fem::PagedArgs* a) {
+  if (!c || !s || !c->k || !c->v || !s->lens || !s->table) return FEM_ERR_NULLPTR;
+  if (tokens && !s->q_start) return FEM_ERR_NULLPTR;
+  if (c->type != FEM_KV_BF16 && (!c->k_scale || !c->v_scale)) return FEM_ERR_NULLPTR;
+  if (c->pages <= 0 || c->heads <= 0 || c->page <= 0 || c->d_qk <= 0 || c->d_v <= 0 ||
+      s->n_seq <= 0 || s->table_len <= 0)
+    return FEM_ERR_SHAPE;
+  if (tokens && (s->n_tok <= 0 || s->max_q <= 0)) return FEM_ERR_SHAPE;
+  if (c->type != FEM_KV_BF16 && c->type != FEM_KV_E4M3 && c->type != FEM_KV_INT8)
+    return FEM_ERR_UNSUPPORTED;
+  if (c->page < 16 || c->page > 1024 || (c->page & (c->page - 1)) != 0) return FEM_ERR_UNSUPPORTED;
+  if (!decode_pair_ok(c->d_qk, c->d_v)) return FEM_ERR_UNSUPPORTED;
+  if ((unsigned long long)c->pages * c->heads > (1ull << 31) ||
+      (unsigned long long)c->pages * c->heads * c->page > (1ull << 40) || c->heads > 65535 ||
+      s->n_seq > 65535 || s->n_tok > (1 << 28) ||
+      (unsigned long long)s->table_len * c->page > (1ull << 30))
+    return FEM_ERR_SHAPE;
+  if (!aligned16(c->k) || !aligned16(c->v)) return FEM_ERR_ALIGN;
+  a->k = static_cast<const uint8_t*>(c->k);
+  a->v = static_cast<const uint8_t*>(c->v);
+  a->ks = c->k_scale;
+  a->vs = c->v_scale;
+  a->q_start = s->q_start;
+  a->lens = s->lens;
+  a->table = s->table;
+  a->pages = c->pages;
+  a->page = c->page;
+  a->page_log2 = __builtin_ctz((unsigned)c->page);
+  a->heads = c->heads;
+  a->nseq = s->n_seq;
+  a->table_len = s->table_len;
+  a->ntok = s->n_tok;
+  a->max_q = s->max_q < s->n_tok ? s->max_q : s->n_tok;
+  return FEM_OK;
+}
+
+// Query heads H of a paged read and the launches' sizes.
+int paged_heads_ok(const fem::PagedArgs& a, int H) {
+  if (H <= 0 || H % a.heads != 0) return FEM_ERR_SHAPE;
+  if ((unsigned long long)a.ntok * H > (1ull << 30)) return FEM_ERR_SHAPE;
+  return FEM_OK;
+}
+constexpr size_t kMostWorkgroups = (size_t)1 << 30;
+
+bool ld_ok(long long ld, long long width) { return ld >= width && ld % 8 == 0; }
 
 }  // namespace
 
@@ -214,6 +263,61 @@ extern "C" int fem_gla_fwd(const void* Q, const void* K, const void* V, const fl
       fem::launch_gla_bf16(Q, K, V, G, beta, out, B, H, T, d_k, d_v, chunk, ws, stream);
   if (e == hipErrorNotSupported) return FEM_ERR_UNSUPPORTED;
   return from_hip(e);
+}
+
+extern "C" int fem_cache_append(const fem_paged_cache* cache, const fem_paged_batch* batch,
+                                const void* k, long long k_ld, const void* v, long long v_ld,
+                                hipStream_t stream) {
+  if (!k || !v) return FEM_ERR_NULLPTR;
+  fem::PagedArgs a;
+  const int rc = paged_args(cache, batch, true, &a);
+  if (rc != FEM_OK) return rc;
+  if (!ld_ok(k_ld, (long long)a.heads * cache->d_qk) || !ld_ok(v_ld, (long long)a.heads * cache->d_v))
+    return FEM_ERR_SHAPE;
+  if (!aligned16(k) || !aligned16(v)) return FEM_ERR_ALIGN;
+  return from_hip(fem::launch_cache_append(a, cache->type, cache->d_qk, cache->d_v, cache->k,
+                                           cache->v, cache->k_scale, cache->v_scale, k, k_ld, v,
+                                           v_ld, stream));
+}
+
+extern "C" int fem_cache_gather(const fem_paged_cache* cache, const fem_paged_batch* batch, void* k,
+                                void* v, int L, hipStream_t stream) {
+  if (!k && !v) return FEM_ERR_NULLPTR;
+  fem::PagedArgs a;
+  const int rc = paged_args(cache, batch, false, &a);
+  if (rc != FEM_OK) return rc;
+  if (L <= 0 || (unsigned long long)a.nseq * a.heads * ((L + 63ull) / 64) > kMostWorkgroups)
+    return FEM_ERR_SHAPE;
+  if ((k && !aligned16(k)) || (v && !aligned16(v))) return FEM_ERR_ALIGN;
+  return from_hip(
+      fem::launch_cache_gather(a, cache->type, cache->d_qk, cache->d_v, k, v, L, stream));
+}
+
+extern "C" size_t fem_paged_workspace_bytes(const fem_paged_cache* cache,
+                                            const fem_paged_batch* batch, int H) {
+  fem::PagedArgs a;
+  if (paged_args(cache, batch, true, &a) != FEM_OK || paged_heads_ok(a, H) != FEM_OK) return 0;
+  return fem::paged_plan(a, H, cache->d_v).ws_bytes;
+}
+
+extern "C" int fem_paged_fwd(const fem_paged_cache* cache, const fem_paged_batch* batch,
+                             const void* q, long long q_ld, const float* beta, void* out, int H,
+                             int flags, void* ws, size_t ws_bytes, hipStream_t stream) {
+  if (!q || !beta || !out) return FEM_ERR_NULLPTR;
+  fem::PagedArgs a;
+  int rc = paged_args(cache, batch, true, &a);
+  if (rc == FEM_OK) rc = paged_heads_ok(a, H);
+  if (rc != FEM_OK) return rc;
+  if (flags & ~(FEM_FLAG_ENCODER | FEM_FLAG_OUT_BF16)) return FEM_ERR_UNSUPPORTED;
+  if (!ld_ok(q_ld, (long long)H * cache->d_qk)) return FEM_ERR_SHAPE;
+  if (!aligned16(q) || !aligned16(out)) return FEM_ERR_ALIGN;
+  const fem::PagedPlan plan = fem::paged_plan(a, H, cache->d_v);
+  if (plan.slots > kMostWorkgroups) return FEM_ERR_SHAPE;
+  rc = check_ws(ws, ws_bytes, plan.ws_bytes);
+  if (rc != FEM_OK) return rc;
+  return from_hip(fem::launch_paged_read(a, plan, cache->type, cache->d_qk, cache->d_v, q, q_ld,
+                                         beta, out, H, !(flags & FEM_FLAG_ENCODER),
+                                         (flags & FEM_FLAG_OUT_BF16) != 0, ws, stream));
 }
 
 extern "C" const char* fem_status_str(int status) {

@@ -87,4 +87,30 @@ hipError_t launch_gla_bf16(const void* Q, const void* K, const void* V, const fl
                            const float* beta, float* out, int B, int H, int T, int dk, int dv,
                            int chunk, void* ws, hipStream_t stream);
 
+// The paged cache (see fem_paged.h): append and gather, and the read.  `kv` is a
+// fem_kv_type, (dk, dv) as launch_softmax_ex_bf16.
+struct PagedArgs;
+hipError_t launch_cache_append(const PagedArgs& a, int kv, int dk, int dv, void* kp, void* vp,
+                               void* ksp, void* vsp, const void* k, long long kld, const void* v,
+                               long long vld, hipStream_t stream);
+hipError_t launch_cache_gather(const PagedArgs& a, int kv, int dk, int dv, void* ko, void* vo, int L,
+                               hipStream_t stream);
+
+// The launches of a read: how many workgroups, and the scratch they need.
+struct PagedPlan {
+  int row_blocks;   // upper bound of the row blocks of a cached head
+  int target;       // splits aimed at, over all heads (0: one a row block)
+  int rps;          // rows of a slot
+  size_t slots, ws_bytes;
+};
+PagedPlan paged_plan(const PagedArgs& a, int H, int dv);
+hipError_t launch_paged_read(const PagedArgs& a, const PagedPlan& plan, int kv, int dk, int dv,
+                             const void* q, long long qld, const float* beta, void* out, int H,
+                             bool causal, bool obf16, void* ws, hipStream_t stream);
+
+struct ReadArgs;
+template <int DK, int DV>
+hipError_t paged_rows(const PagedArgs& a, const ReadArgs& r, const PagedPlan& plan, int kv,
+                      hipStream_t stream);
+
 }  // namespace fem

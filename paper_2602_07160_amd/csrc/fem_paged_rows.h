@@ -1,0 +1,706 @@
+// The FEM read of few query rows over a paged cache: one decoding token, a
+// group of query heads, a handful of drafted tokens.
+//
+//   out_j = (1/beta_j) [ log sum_i exp(s_i + beta_j v_ij) - log sum_i exp(s_i) ]
+//
+// The rows that share a cached head (tokens of a sequence times query heads of
+// the group) are read together, up to 32 at a time, so that the cache is read
+// once for all of them.
+//
+// Work.  The keys of a row block are split over workgroups (below) and, inside
+// one, dealt to its four waves in tiles of 32 keys.  A wave works alone, with
+// no barrier until its last tile: its scores, running row maxima, tilted
+// values and running column shifts are its own.
+//
+//   * S^T = K Q^T on v_mfma_f32_16x16x32_bf16, K's fragments loaded straight
+//     from the cache (a lane holds 8 dimensions of one key);
+//   * P = 2^(s - m + 40), m a row maximum raised only past a lag of 8;
+//   * V goes through the wave's own LDS area and comes back transposed
+//     (ds_read_tr16_b64), so that a lane holds eight keys of one channel:
+//     E = 2^(beta log2e v - c + 40), c a channel's shift raised likewise,
+//     formed once for all rows; bf16, hi + lo where beta < 0.5;
+//   * O += P E with P's registers as the scores left them (the contraction's
+//     key order is permuted the same way on both sides).
+//   * The next tile's K and V are loaded into the registers that this tile's
+//     products and LDS writes have just freed, so a whole tilt hides them.
+//
+// What bounds it: HBM (a tile of 32 keys at d = 128 moves 16 KiB for ~2700
+// vector cycles of tilt on one of a compute unit's four SIMDs).
+//
+// Range.  P and E carry a bias of 40 and a lag of 8 each: their product is at
+// most 2^96, and a term that underflows in either factor is at most 2^-70 of
+// the frame (m, c), so a sum of at least 2^-40 has lost nothing that fp32 would
+// keep.  A smaller sum (every visible key with a large score has a small value
+// and the other way round, by 120 octaves together) is formed again, exactly,
+// from the keys of the workgroup's range.
+#pragma once
+
+#include "fem_internal.h"
+#include "fem_paged.h"
+
+namespace fem {
+
+constexpr int kRowsMax = 32;       // query rows of a block
+constexpr int kRowTile = 32;       // keys of a wave's tile
+constexpr int kRowWaves = 4;
+constexpr int kRowThreads = 64 * kRowWaves;
+constexpr float kRowBias = 40.f;   // of P and of E
+constexpr float kLag = 8.f;        // of m and of c
+constexpr float kLoBelow = 0.5f;   // channels with beta below this take E as hi + lo
+
+// ---- who does what ------------------------------------------------------------
+
+// The split of a call's work, formed by every wave from the lengths: sequence
+// b has nrb row blocks and nt key tiles; tps tiles make a split, so that all
+// splits of all heads number at most `target` + one a row block and head.
+struct RowItem {
+  int b, rb, s, ns;  // sequence, row block, split and the number of splits
+  int slot;          // of split s of head 0 among the heads' slots
+  Seq seq;
+  bool found;
+};
+
+struct RowCounts {
+  int nrb, nt;
+};
+
+__device__ __forceinline__ RowCounts row_counts(const Seq& q, int G, int max_q) {
+  RowCounts c;
+  const bool ok = q.ok && q.n <= max_q;
+  c.nrb = (int)(((long long)q.n * G + kRowsMax - 1) / kRowsMax);
+  c.nt = ok ? max((q.len + kRowTile - 1) / kRowTile, 1) : 1;
+  return c;
+}
+
+__device__ __forceinline__ long long wave_sum64(long long x) {
+  for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o);
+  return x;
+}
+
+// Tiles of a split.
+__device__ __forceinline__ int tiles_per_split(const PagedArgs& a, int G, bool causal, int target) {
+  if (target == 0) return 1 << 30;  // one split each
+  const int lane = threadIdx.x & 63;
+  long long t = 0;
+  for (int b0 = 0; b0 < a.nseq; b0 += 64) {
+    const int b = b0 + lane;
+    if (b < a.nseq) {
+      const RowCounts c = row_counts(seq_of(a, b, causal), G, a.max_q);
+      t += (long long)c.nrb * c.nt;
+    }
+  }
+  t = wave_sum64(t) * a.heads;
+  const long long tps = (t + target - 1) / target;
+  return (int)min(max(tps, (long long)kRowWaves), 1ll << 30);
+}
+
+// Item `x` of all heads' alike: a split of a row block (SPLITS), or a whole
+// row block.  Items are numbered by sequence, row block and split.
+template <bool SPLITS>
+__device__ __forceinline__ RowItem find_item(const PagedArgs& a, int G, bool causal, int tps, int x) {
+  const int lane = threadIdx.x & 63;
+  RowItem it;
+  it.found = false;
+  int base = 0, slot = 0;
+  for (int b0 = 0; b0 < a.nseq; b0 += 64) {
+    const int b = b0 + lane;
+    int ns = 1, nrb = 0;
+    if (b < a.nseq) {
+      const RowCounts c = row_counts(seq_of(a, b, causal), G, a.max_q);
+      nrb = c.nrb;
+      ns = (c.nt + tps - 1) / tps;
+    }
+    const int mine = SPLITS ? nrb * ns : nrb, slots = nrb * ns;
+    int end = mine, send = slots;
+    for (int o = 1; o < 64; o <<= 1) {
+      const int u = __shfl_up(end, o), w = __shfl_up(send, o);
+      if (lane >= o) {
+        end += u;
+        send += w;
+      }
+    }
+    const uint64_t m = __ballot(base + end > x);
+    if (m != 0) {
+      const int l = __builtin_ctzll(m);
+      it.found = true;
+      it.b = b0 + l;
+      const int first = base + __shfl(end - mine, l);
+      it.ns = __shfl(ns, l);
+      const int at = x - first;
+      it.rb = SPLITS ? at / it.ns : at;
+      it.s = SPLITS ? at % it.ns : 0;
+      it.slot = slot + __shfl(send - slots, l) + it.rb * it.ns + it.s;
+      break;
+    }
+    base += __shfl(end, 63);
+    slot += __shfl(send, 63);
+  }
+  if (it.found) {
+    it.b = __builtin_amdgcn_readfirstlane(it.b);
+    it.seq = seq_of(a, it.b, causal);
+    it.seq.ok = it.seq.ok && it.seq.n <= a.max_q;
+  }
+  return it;
+}
+
+// Keys that row r of a sequence's group sees.
+__device__ __forceinline__ int row_limit(const Seq& s, int r, int G, bool causal) {
+  return causal ? s.len - s.n + r / G + 1 : s.len;
+}
+
+// ---- exact form ---------------------------------------------------------------
+
+// log2 sum over keys [k0, k1) of 2^(s_i + bl v_ij), formed by a whole wave in
+// fp32; returns -inf for no keys.
+template <int DK, int DV, int KV>
+__device__ float exact_joint(const PagedArgs& a, const bf16* qrow, int b, int g, int j, float bl,
+                             int k0, int k1, float scale2) {
+  Lse2 t;
+  for (int i = k0 + (threadIdx.x & 63); i < k1; i += 64) {
+    bool bad = false;
+    const size_t row = paged_row(a, b, g, i, bad);
+    float dot = 0.f;
+    for (int c = 0; c < DK / 8; ++c) {
+      const bf16x8 x = reinterpret_cast<const bf16x8*>(qrow)[c];
+      float f[8];
+      row8<KV, DK>(a.k, a.ks, row, c, f);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) dot = fmaf((float)x[e], f[e], dot);
+    }
+    float f[8], v = 0.f;
+    row8<KV, DV>(a.v, a.vs, row, j >> 3, f);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v = (j & 7) == e ? f[e] : v;
+    t.add(fmaf(v, bl, dot * scale2));
+  }
+  return t.wave_total();
+}
+
+// ---- the read -------------------------------------------------------------------
+
+template <int DK, int DV>
+struct RowCfg {
+  static constexpr int NKS = DK / 32;          // k-steps of K Q^T
+  static constexpr int NCB = DV / 16;          // 16-channel blocks
+  static constexpr int VROW = DV * 2 + 32;     // LDS row of a V tile (bytes): conflict-free
+  static constexpr int VT = kRowTile * VROW;   // a wave's V area
+  static constexpr int OROW = DV + 4;          // LDS row of a merge area (floats)
+  static constexpr int MT = 16 * OROW * 4;     // a wave's merge area
+  static constexpr int AREA = VT > MT ? VT : MT;
+};
+
+// Stored bytes of a tile in registers.
+template <int W, int KV>
+struct Stored {
+  // K: per 16-key block and k-step (32 channels), 8 values of the lane's key
+  // V: per 16-key block, 16-byte pieces in memory order
+  static constexpr int KN = W / 32;
+  static constexpr int VN = KV == FEM_KV_BF16 ? W / 32 : (W + 63) / 64;
+};
+
+template <int DK, int DV, int KV, int RB>
+struct RowRead {
+  using C = RowCfg<DK, DV>;
+  static constexpr bool MX = KV != FEM_KV_BF16;
+  static constexpr int KN = C::NKS;                       // K pieces of a block
+  static constexpr int VN = MX ? (DV + 63) / 64 : DV / 32;  // V pieces of a block
+
+  typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+
+  const PagedArgs& a;
+  int b, g, n_eff;  // sequence, cached head, keys the block may see at all
+  int lane, l16, grp;
+  unsigned char* vt;  // this wave's LDS area
+  bool bad = false;
+
+  bf16x8 qf[RB][C::NKS];
+  f32x4 acc[RB][C::NCB];
+  float m[RB], lsum[RB];
+  float bl[C::NCB], c[C::NCB];
+  unsigned lo_blocks;  // bit cb: a channel of the block takes hi + lo
+
+  u32x4 kw[2][KN];        // bf16: 8 values; 8-bit: words 0, 1 hold 8 codes
+  unsigned ksc[2][KN];
+  u32x4 vw[2][VN];
+  unsigned vsc[2][VN];
+
+  __device__ __forceinline__ RowRead(const PagedArgs& a_) : a(a_) {}
+
+  // First row of the 16-key block at key k (inside one page), clamped to the
+  // last block that has visible keys.
+  __device__ __forceinline__ size_t block_row(int k) {
+    const int kk = min(k, (n_eff - 1) & ~15);
+    int p = a.table[(size_t)b * a.table_len + (kk >> a.page_log2)];
+    p = __builtin_amdgcn_readfirstlane(p);
+    if ((unsigned)p >= (unsigned)a.pages) {
+      bad = true;
+      p = 0;
+    }
+    return (((size_t)p * a.heads + g) << a.page_log2) + (kk & (a.page - 1));
+  }
+
+  __device__ __forceinline__ void load_k(const size_t (&row)[2]) {
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb) {
+      if constexpr (!MX) {
+        const uint8_t* p = a.k + row[kb] * (DK * 2);
+#pragma unroll
+        for (int ks = 0; ks < KN; ++ks)
+          kw[kb][ks] = *reinterpret_cast<const u32x4*>(p + l16 * (DK * 2) + ks * 64 + grp * 16);
+      } else {
+        const uint8_t* p = a.k + row[kb] * DK;
+        const uint8_t* sp = a.ks + row[kb] * (DK / kScaleBlock);
+#pragma unroll
+        for (int ks = 0; ks < KN; ++ks) {
+          const u32x2v w = *reinterpret_cast<const u32x2v*>(p + l16 * DK + ks * 32 + grp * 8);
+          kw[kb][ks][0] = w[0];
+          kw[kb][ks][1] = w[1];
+          ksc[kb][ks] = sp[l16 * (DK / kScaleBlock) + ks];
+        }
+      }
+    }
+  }
+  __device__ __forceinline__ void load_v(const size_t (&row)[2]) {
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb) {
+      if constexpr (!MX) {
+        const uint8_t* p = a.v + row[kb] * (DV * 2);
+#pragma unroll
+        for (int i = 0; i < VN; ++i)
+          vw[kb][i] = *reinterpret_cast<const u32x4*>(p + (i * 64 + lane) * 16);
+      } else {
+        const uint8_t* p = a.v + row[kb] * DV;
+        const uint8_t* sp = a.vs + row[kb] * (DV / kScaleBlock);
+#pragma unroll
+        for (int i = 0; i < VN; ++i) {
+          const int piece = DV == 32 ? lane & 31 : i * 64 + lane;  // of 16 codes
+          vw[kb][i] = *reinterpret_cast<const u32x4*>(p + piece * 16);
+          vsc[kb][i] = sp[piece >> 1];
+        }
+      }
+    }
+  }
+  __device__ __forceinline__ bf16x8 k_frag(int kb, int ks) const {
+    if constexpr (!MX) return __builtin_bit_cast(bf16x8, kw[kb][ks]);
+    return __builtin_bit_cast(bf16x8, dequant8<KV>(kw[kb][ks][0], kw[kb][ks][1],
+                                                   scale_of(ksc[kb][ks])));
+  }
+  // The tile's V into LDS as [32][DV] bf16; rows at or past `live` become -inf
+  // (E = 0 there, and the column maximum does not see them).
+  __device__ __forceinline__ void store_v(int live) {
+    constexpr unsigned kNegInf2 = 0xff80ff80u;
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb) {
+#pragma unroll
+      for (int i = 0; i < VN; ++i) {
+        if constexpr (!MX) {
+          constexpr int PPR = DV / 8;  // pieces of a row
+          const int piece = i * 64 + lane, row = kb * 16 + piece / PPR, col = piece % PPR;
+          u32x4 w = vw[kb][i];
+          if (live < kRowTile && row >= live) w = u32x4{kNegInf2, kNegInf2, kNegInf2, kNegInf2};
+          *reinterpret_cast<u32x4*>(vt + row * C::VROW + col * 16) = w;
+        } else {
+          constexpr int PPR = DV / 16;
+          const int piece = DV == 32 ? lane & 31 : i * 64 + lane;
+          const int row = kb * 16 + piece / PPR, col = piece % PPR;
+          const float s = scale_of(vsc[kb][i]);
+          u32x4 w0 = dequant8<KV>(vw[kb][i][0], vw[kb][i][1], s);
+          u32x4 w1 = dequant8<KV>(vw[kb][i][2], vw[kb][i][3], s);
+          if (live < kRowTile && row >= live) {
+            w0 = u32x4{kNegInf2, kNegInf2, kNegInf2, kNegInf2};
+            w1 = w0;
+          }
+          u32x4* d = reinterpret_cast<u32x4*>(vt + row * C::VROW + col * 32);
+          d[0] = w0;
+          d[1] = w1;
+        }
+      }
+    }
+  }
+
+  // One tile of keys k0 .. k0+31.  `masked`: some row does not see all of it;
+  // lim[rb]: keys that the lane's row sees.  The next tile's rows are loaded
+  // where `more` is set.
+  __device__ __forceinline__ void tile(int k0, bool masked, const int (&lim)[RB], bool more,
+                                       int knext, float scale2) {
+    // ---- S^T = K Q^T
+    f32x4 s[RB][2];
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) s[rb][0] = s[rb][1] = f32x4{};
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb) {
+#pragma unroll
+      for (int ks = 0; ks < KN; ++ks) {
+        const bf16x8 kf = k_frag(kb, ks);
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb)
+          s[rb][kb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[rb][ks], s[rb][kb], 0, 0, 0);
+      }
+    }
+    store_v(n_eff - k0);
+    if (more) {
+      const size_t row[2] = {block_row(knext), block_row(knext + 16)};
+      load_k(row);
+      load_v(row);
+    }
+
+    // ---- P, in the A operand's layout: row l16, keys 4 grp + i, 16 + 4 grp + i
+    bf16x8 p[RB];
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+      float x[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] = s[rb][e >> 2][e & 3] * scale2;
+      if (masked) {
+        const int left = lim[rb] - k0 - 4 * grp;
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if ((e & 3) + 16 * (e >> 2) >= left) x[e] = -INFINITY;
+      }
+      float mx = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])),
+                       fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
+      if (__any(mx > m[rb] + kLag)) {
+        mx = fmaxf(mx, __shfl_xor(mx, 16));
+        mx = fmaxf(mx, __shfl_xor(mx, 32));
+        const float mn = mx > m[rb] + kLag ? mx : m[rb];
+        const float f = mn == m[rb] ? 1.f : exp2_hw(m[rb] - mn);
+        m[rb] = mn;
+        lsum[rb] *= f;
+        f32x4 fr;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) fr[i] = __shfl(f, 4 * grp + i);
+#pragma unroll
+        for (int cb = 0; cb < C::NCB; ++cb) acc[rb][cb] *= fr;
+      }
+      // a row that has seen no key yet keeps m = -inf: a finite stand-in
+      const float sh = kRowBias - fmaxf(m[rb], -3e38f);
+#pragma unroll
+      for (int e = 0; e < 8; e += 2) {
+        // rounded to bf16 (2^-9 relative); lsum adds the same rounded values,
+        // so the rounding cancels from the mean over the keys
+        const bf16x2 p2 = to_bf16x2(exp2_hw(x[e] + sh), exp2_hw(x[e + 1] + sh));
+        p[rb][e] = p2[0];
+        p[rb][e + 1] = p2[1];
+        lsum[rb] = add_bf16x2(p2, lsum[rb]);
+      }
+    }
+
+    // ---- E and O += P E, 16 channels at a time
+    const int tr = (4 * grp + (l16 >> 2)) * C::VROW + (l16 & 3) * 8;
+#pragma unroll
+    for (int cb = 0; cb < C::NCB; ++cb) {
+      const s16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(vt + tr + cb * 32));
+      const s16x4 v1 =
+          __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(vt + tr + 16 * C::VROW + cb * 32));
+      float v[8];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        v[e] = __uint_as_float((unsigned)(unsigned short)v0[e] << 16);
+        v[4 + e] = __uint_as_float((unsigned)(unsigned short)v1[e] << 16);
+      }
+      const float vx = fmaxf(fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])),
+                             fmaxf(fmaxf(v[4], v[5]), fmaxf(v[6], v[7])));
+      if (__any(vx * bl[cb] > c[cb] + kLag)) {
+        float mx = fmaxf(vx, __shfl_xor(vx, 16));
+        mx = fmaxf(mx, __shfl_xor(mx, 32)) * bl[cb];
+        const float cn = mx > c[cb] + kLag ? mx : c[cb];
+        const float f = cn == c[cb] ? 1.f : exp2_hw(c[cb] - cn);
+        c[cb] = cn;
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) acc[rb][cb] *= f;
+      }
+      const float sh = kRowBias - c[cb];
+      float e8[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) e8[e] = exp2_hw(fmaf(v[e], bl[cb], sh));
+      if ((lo_blocks >> cb) & 1) {
+        // beta < 0.5 turns a rounding of E to bf16 into more than 2^-8 of the
+        // read: E = hi (truncated) + lo (the rest, rounded), 2^-16 relative
+        bf16x8 hi, lo;
+#pragma unroll
+        for (int e = 0; e < 8; e += 2) {
+          const unsigned u0 = __float_as_uint(e8[e]), u1 = __float_as_uint(e8[e + 1]);
+          const bf16x2 h = __builtin_bit_cast(bf16x2, __builtin_amdgcn_perm(u1, u0, 0x07060302u));
+          const bf16x2 l = to_bf16x2(e8[e] - __uint_as_float(u0 & 0xffff0000u),
+                                     e8[e + 1] - __uint_as_float(u1 & 0xffff0000u));
+          hi[e] = h[0];
+          hi[e + 1] = h[1];
+          lo[e] = l[0];
+          lo[e + 1] = l[1];
+        }
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) {
+          acc[rb][cb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(p[rb], hi, acc[rb][cb], 0, 0, 0);
+          acc[rb][cb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(p[rb], lo, acc[rb][cb], 0, 0, 0);
+        }
+      } else {
+        bf16x8 hi;
+#pragma unroll
+        for (int e = 0; e < 8; e += 2) {
+          const bf16x2 h = to_bf16x2(e8[e], e8[e + 1]);
+          hi[e] = h[0];
+          hi[e + 1] = h[1];
+        }
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb)
+          acc[rb][cb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(p[rb], hi, acc[rb][cb], 0, 0, 0);
+      }
+    }
+  }
+};
+
+// Arguments of a read besides the cache and the sequences.
+struct ReadArgs {
+  const bf16* q;       // token t, head h at t * qld + h * DK
+  long long qld;
+  const float* beta;   // [heads][DV]
+  void* out;           // [ntok][H][DV] float32 or bf16
+  float* part;         // [slot][rps][DV + 1]: log2 joint sums, then the row's log2 normaliser
+  int H, G;            // query heads, of a cached head
+  int rps;             // rows of a slot
+  int target;          // see tiles_per_split
+  int causal, obf16;
+};
+
+__device__ __forceinline__ void put(const ReadArgs& r, size_t at, float x) {
+  if (r.obf16) static_cast<bf16*>(r.out)[at] = (bf16)x;
+  else static_cast<float*>(r.out)[at] = x;
+}
+
+// The read of one split of one row block (at most 16 RB rows) of cached head g.
+template <int DK, int DV, int KV, int RB>
+__device__ __forceinline__ void rows_body(const PagedArgs& a, const ReadArgs& r, const RowItem& it,
+                                          int g, int slot, unsigned char* smem) {
+  using C = RowCfg<DK, DV>;
+  RowRead<DK, DV, KV, RB> w(a);
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  w.lane = tid & 63;
+  w.l16 = tid & 15;
+  w.grp = (tid & 63) >> 4;
+  w.vt = smem + wave * C::AREA;
+  w.b = it.b;
+  w.g = g;
+  const Seq& sq = it.seq;
+  const bool causal = r.causal != 0;
+  const int r0 = it.rb * kRowsMax, nr = min((int)min((long long)sq.n * r.G - r0, 32ll), 16 * RB);
+  w.n_eff = row_limit(sq, r0 + nr - 1, r.G, causal);
+  const int tiles = (w.n_eff + kRowTile - 1) / kRowTile;
+  const int tb = (int)((long long)it.s * tiles / it.ns);
+  const int te = (int)((long long)(it.s + 1) * tiles / it.ns);
+  const float scale2 = kLog2e / sqrtf((float)DK);
+
+  int t = tb + wave;
+  if (t < te) {
+    const size_t row[2] = {w.block_row(t * kRowTile), w.block_row(t * kRowTile + 16)};
+    w.load_k(row);
+    w.load_v(row);
+  }
+  int lim[RB];
+  int least = 0x7fffffff;  // keys that every row sees
+#pragma unroll
+  for (int rb = 0; rb < RB; ++rb) {
+    const int row = r0 + min(rb * 16 + w.l16, nr - 1);  // rows past the last repeat it
+    const int tok = row / r.G, h = g * r.G + row % r.G;
+    const bf16* qp = r.q + (size_t)(sq.q0 + tok) * (size_t)r.qld + (size_t)h * DK + w.grp * 8;
+#pragma unroll
+    for (int ks = 0; ks < C::NKS; ++ks) w.qf[rb][ks] = *reinterpret_cast<const bf16x8*>(qp + ks * 32);
+    lim[rb] = row_limit(sq, row, r.G, causal);
+    w.m[rb] = -INFINITY;
+    w.lsum[rb] = 0.f;
+#pragma unroll
+    for (int cb = 0; cb < C::NCB; ++cb) w.acc[rb][cb] = f32x4{};
+  }
+  least = row_limit(sq, r0, r.G, causal);
+  w.lo_blocks = 0;
+#pragma unroll
+  for (int cb = 0; cb < C::NCB; ++cb) {
+    const float b = r.beta[g * DV + cb * 16 + w.l16];
+    w.bl[cb] = b * kLog2e;
+    w.c[cb] = -INFINITY;
+    if (__any(!(b >= kLoBelow))) w.lo_blocks |= 1u << cb;
+  }
+  for (; t < te; t += kRowWaves) {
+    const int k0 = t * kRowTile;
+    w.tile(k0, k0 + kRowTile > least, lim, t + kRowWaves < te, (t + kRowWaves) * kRowTile, scale2);
+  }
+
+  // ---- the four waves meet: common frames M (row) and Cc (channel)
+  float* const fm = reinterpret_cast<float*>(smem + kRowWaves * C::AREA);  // [4][32] row maxima
+  float* const fl = fm + kRowWaves * kRowsMax;                            // [4][32] row sums
+  float* const fc = fl + kRowWaves * kRowsMax;                            // [4][DV] shifts
+  int* const fbad = reinterpret_cast<int*>(fc + kRowWaves * DV);           // [4]
+#pragma unroll
+  for (int rb = 0; rb < RB; ++rb) {
+    float l = w.lsum[rb];
+    l += __shfl_xor(l, 16);
+    l += __shfl_xor(l, 32);
+    if (w.grp == 0) {
+      fm[wave * kRowsMax + rb * 16 + w.l16] = w.m[rb];
+      fl[wave * kRowsMax + rb * 16 + w.l16] = l;
+    }
+  }
+  if (w.grp == 0) {
+#pragma unroll
+    for (int cb = 0; cb < C::NCB; ++cb) fc[wave * DV + cb * 16 + w.l16] = w.c[cb];
+  }
+  if (w.lane == 0) fbad[wave] = w.bad;
+  __syncthreads();
+  const bool bad = (fbad[0] | fbad[1] | fbad[2] | fbad[3]) != 0;
+  auto top4 = [](const float* p, int stride) {
+    return fmaxf(fmaxf(p[0], p[stride]), fmaxf(p[2 * stride], p[3 * stride]));
+  };
+  float cf[C::NCB];
+#pragma unroll
+  for (int cb = 0; cb < C::NCB; ++cb) {
+    const float top = top4(fc + cb * 16 + w.l16, DV);
+    cf[cb] = w.c[cb] == -INFINITY ? 0.f : exp2_hw(w.c[cb] - top);
+  }
+#pragma unroll
+  for (int rb = 0; rb < RB; ++rb) {
+    if (rb > 0) __syncthreads();
+    f32x4 rf;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int q = rb * 16 + 4 * w.grp + i;
+      const float mine = fm[wave * kRowsMax + q];
+      rf[i] = mine == -INFINITY ? 0.f : exp2_hw(mine - top4(fm + q, kRowsMax));
+    }
+    float* area = reinterpret_cast<float*>(smem + wave * C::AREA);
+#pragma unroll
+    for (int cb = 0; cb < C::NCB; ++cb) {
+      const f32x4 x = w.acc[rb][cb] * rf * cf[cb];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) area[(4 * w.grp + i) * C::OROW + cb * 16 + w.l16] = x[i];
+    }
+    __syncthreads();
+    const int kbeg = tb * kRowTile, kend = min(te * kRowTile, w.n_eff);
+    for (int e = tid; e < 16 * DV; e += kRowThreads) {
+      const int q = e / DV, j = e % DV, row = r0 + rb * 16 + q;
+      if (rb * 16 + (e & ~63) / DV >= nr) break;  // the wave's rows are past the last
+      const bool live = rb * 16 + q < nr;
+      const float M = top4(fm + rb * 16 + q, kRowsMax), top = top4(fc + j, DV);
+      float sum = 0.f, l = 0.f;
+#pragma unroll
+      for (int x = 0; x < kRowWaves; ++x) {
+        sum += reinterpret_cast<const float*>(smem + x * C::AREA)[q * C::OROW + j];
+        const float mx = fm[x * kRowsMax + rb * 16 + q];
+        l += mx == -INFINITY ? 0.f : fl[x * kRowsMax + rb * 16 + q] * exp2_hw(mx - M);
+      }
+      const float blj = r.beta[g * DV + j] * kLog2e;
+      const int seen = min(kend, row_limit(sq, row, r.G, causal));  // of this range, up to here
+      const bool none = !live || seen <= kbeg;
+      float y = none ? -INFINITY : log2_hw(sum) + (M + top - 2.f * kRowBias);
+      const float lp = none ? -INFINITY : log2_hw(l) + (M - kRowBias);
+      bool redo = !none && !bad && !(sum >= 0x1p-40f);
+      uint64_t who = __ballot(redo);
+      while (who != 0) {
+        const int src = __builtin_ctzll(who);
+        who &= who - 1;
+        const int rr = __builtin_amdgcn_readlane(row, src), jj = __builtin_amdgcn_readlane(j, src);
+        const int ee = __builtin_amdgcn_readlane(seen, src);
+        const bf16* qp = r.q + (size_t)(sq.q0 + rr / r.G) * (size_t)r.qld +
+                         (size_t)(g * r.G + rr % r.G) * DK;
+        const float x = exact_joint<DK, DV, KV>(a, qp, it.b, g, jj, r.beta[g * DV + jj] * kLog2e,
+                                                kbeg, ee, scale2);
+        if (w.lane == src) y = x;
+      }
+      if (!live) continue;
+      if (it.ns == 1) {
+        // one logarithm of a ratio near 1 where the sums allow it
+        const float x = sum / l * 0x1p-40f;
+        float o = !redo && x >= 0x1p-120f ? (log2_hw(x) + top) / blj : (y - lp) / blj;
+        if (bad) o = NAN;
+        put(r, ((size_t)(sq.q0 + row / r.G) * r.H + g * r.G + row % r.G) * DV + j, o);
+      } else {
+        float* p = r.part + ((size_t)slot * r.rps + rb * 16 + q) * (DV + 1);
+        p[j] = bad ? NAN : y;
+        if (j == 0) p[DV] = bad ? NAN : lp;
+      }
+    }
+  }
+}
+
+// Workgroup x * heads + g: item x of cached head g.
+template <int DK, int DV, int KV>
+__global__ __launch_bounds__(kRowThreads, 2) void paged_rows_kernel(PagedArgs a, ReadArgs r) {
+  using C = RowCfg<DK, DV>;
+  __shared__ __align__(16) unsigned char
+      smem[kRowWaves * C::AREA + kRowWaves * (2 * kRowsMax + DV) * 4 + 16];
+  const int g = blockIdx.x % a.heads, x = blockIdx.x / a.heads;
+  const bool causal = r.causal != 0;
+  const int tps = tiles_per_split(a, r.G, causal, r.target);
+  const RowItem it = find_item<true>(a, r.G, causal, tps, x);
+  if (!it.found) return;
+  const int r0 = it.rb * kRowsMax, nr = min((int)min((long long)it.seq.n * r.G - r0, 32ll), 32);
+  if (!it.seq.ok || it.seq.len == 0) {  // nothing can be read, or there is nothing to read
+    for (int e = threadIdx.x; e < nr * DV; e += kRowThreads) {
+      const int row = r0 + e / DV;
+      put(r, ((size_t)(it.seq.q0 + row / r.G) * r.H + g * r.G + row % r.G) * DV + e % DV, NAN);
+    }
+    return;
+  }
+  if (nr <= 16) rows_body<DK, DV, KV, 1>(a, r, it, g, (int)blockIdx.x, smem);
+  else rows_body<DK, DV, KV, 2>(a, r, it, g, (int)blockIdx.x, smem);
+}
+
+// Merge of the splits of row block x, cached head g.  The workgroup's threads
+// are groups of DV; few rows share the groups over the splits, many take a
+// group each.
+constexpr int kMergeThreads = 512;
+
+template <int DV>
+__global__ __launch_bounds__(kMergeThreads) void paged_merge_kernel(PagedArgs a, ReadArgs r) {
+  constexpr int NG = kMergeThreads / DV;
+  __shared__ float4 part[NG][DV];
+  const int g = blockIdx.x % a.heads, x = blockIdx.x / a.heads;
+  const bool causal = r.causal != 0;
+  const int tps = tiles_per_split(a, r.G, causal, r.target);
+  const RowItem it = find_item<false>(a, r.G, causal, tps, x);
+  if (!it.found || it.ns == 1) return;
+  const int r0 = it.rb * kRowsMax, nr = min((int)min((long long)it.seq.n * r.G - r0, 32ll), 32);
+  int per = NG;  // groups of a row
+  while (per > 1 && (NG / per) < nr) per >>= 1;
+  const int rows = NG / per;  // rows at a time
+  const int grp = threadIdx.x / DV, j = threadIdx.x % DV;
+  const float blj = r.beta[g * DV + j] * kLog2e;
+  for (int q0 = 0; q0 < nr; q0 += rows) {
+    const int q = q0 + grp / per, sub = grp % per;
+    float M = -INFINITY, S = 0.f, md = -INFINITY, sd = 0.f;
+    auto join = [](float& m, float& s, float m2, float s2) {
+      const float mn = fmaxf(m, m2);
+      if (mn == -INFINITY) {  // nothing yet, or NaN, which the sum keeps
+        s += s2;
+        return;
+      }
+      s = s * exp2_hw(m - mn) + s2 * exp2_hw(m2 - mn);
+      m = mn;
+    };
+    // 2^x / 2^x of a partial sum's logarithm x: 0 of none, NaN of NaN (which
+    // the maxima pass over, so the sums carry it)
+    auto one = [](float x) { return x == -INFINITY ? 0.f : x != x ? x : 1.f; };
+    if (q < nr) {
+#pragma unroll 4
+      for (int s = sub; s < it.ns; s += per) {
+        const float* p =
+            r.part + ((size_t)((size_t)(it.slot + s) * a.heads + g) * r.rps + q) * (DV + 1);
+        join(M, S, p[j], one(p[j]));
+        join(md, sd, p[DV], one(p[DV]));
+      }
+    }
+    part[grp][j] = make_float4(M, S, md, sd);
+    __syncthreads();
+    if (q < nr && sub == 0) {
+      for (int u = 1; u < per; ++u) {
+        const float4 o = part[grp + u][j];
+        join(M, S, o.x, o.y);
+        join(md, sd, o.z, o.w);
+      }
+      const float o = ((M - md) + (log2_hw(S) - log2_hw(sd))) / blj;
+      const int row = r0 + q;
+      put(r, ((size_t)(it.seq.q0 + row / r.G) * r.H + g * r.G + row % r.G) * DV + j, o);
+    }
+    __syncthreads();
+  }
+}
+
+}  // namespace fem

@@ -1,0 +1,10 @@
+// Few-row paged reads at d_qk = 128 (fem_paged_rows.h).
+
+#include "fem_paged_launch.h"
+
+namespace fem {
+
+template hipError_t paged_rows<128, 64>(const PagedArgs&, const ReadArgs&, const PagedPlan&, int,
+                                         hipStream_t);
+
+}  // namespace fem
