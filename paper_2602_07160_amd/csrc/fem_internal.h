@@ -98,10 +98,16 @@ hipError_t launch_cache_gather(const PagedArgs& a, int kv, int dk, int dv, void*
 
 // The launches of a read: how many workgroups, and the scratch they need.
 struct PagedPlan {
-  int row_blocks;   // upper bound of the row blocks of a cached head
-  int target;       // splits aimed at, over all heads (0: one a row block)
-  int rps;          // rows of a slot
-  size_t slots, ws_bytes;
+  bool rows, wide;         // whether the kernel for few rows runs, and the one for many
+  long long most_rows;     // sequences of the first: rows <= most_rows, of the second:
+  long long wide_least;    //   rows > wide_least
+  int row_blocks, target;  // few rows: bound of the row blocks of a cached head, and the
+                           //   splits aimed at over all heads (0: one a row block)
+  int wide_blocks;         // many rows: bound of a cached head's row blocks
+  bool split_wide;
+  int rps, wide_rps;       // rows of a slot
+  size_t slots;            // workgroups and slots of the first kernel
+  size_t part_at, wide_at, ws_bytes;
 };
 PagedPlan paged_plan(const PagedArgs& a, int H, int dv);
 hipError_t launch_paged_read(const PagedArgs& a, const PagedPlan& plan, int kv, int dk, int dv,
@@ -111,6 +117,9 @@ hipError_t launch_paged_read(const PagedArgs& a, const PagedPlan& plan, int kv, 
 struct ReadArgs;
 template <int DK, int DV>
 hipError_t paged_rows(const PagedArgs& a, const ReadArgs& r, const PagedPlan& plan, int kv,
+                      hipStream_t stream);
+template <int DK, int DV>
+hipError_t paged_wide(const PagedArgs& a, const ReadArgs& r, const PagedPlan& plan, int kv,
                       hipStream_t stream);
 
 }  // namespace fem

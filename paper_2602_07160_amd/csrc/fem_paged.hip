@@ -1,50 +1,86 @@
-// The paged FEM read: how a call's work is split, and its launches.
+// The paged FEM read: which kernels a call takes, and their scratch.
 
 #include "fem_internal.h"
-#include "fem_paged_rows.h"
+#include "fem_paged_wide.h"
 
 #include <algorithm>
 
 namespace fem {
 
 namespace {
-constexpr int kTarget = 1024;   // splits aimed at
-constexpr int kShortKeys = 128; // contexts that one workgroup reads in one round
+constexpr int kTarget = 1024;    // splits of few rows aimed at
+constexpr int kShortKeys = 128;  // contexts that one workgroup reads in one round
+
+size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 }  // namespace
 
+// Up to 32 rows a sequence the kernel for few rows; more, the one for many; both
+// where max_q allows either.
 PagedPlan paged_plan(const PagedArgs& a, int H, int dv) {
-  PagedPlan p;
+  PagedPlan p = {};
   const long long G = H / a.heads, rows = (long long)a.ntok * G, most = a.max_q * G;
-  const long long blocks = std::min(rows / kRowsMax + a.nseq,
-                                    (most + kRowsMax - 1) / kRowsMax * (long long)a.nseq);
-  p.row_blocks = (int)std::min(blocks, 1ll << 30);
-  p.target = ((long long)a.table_len << a.page_log2) <= kShortKeys ? 0 : kTarget;
-  p.rps = (int)std::min<long long>(kRowsMax, most);
-  p.slots = (size_t)p.target + (size_t)p.row_blocks * a.heads;
-  p.ws_bytes = p.target ? p.slots * p.rps * (dv + 1) * sizeof(float) : 0;
+  const long long keys = (long long)a.table_len << a.page_log2;
+  auto blocks = [&](long long most_, int br) {
+    return (int)std::min(rows / br + a.nseq, (most_ + br - 1) / br * (long long)a.nseq);
+  };
+  p.wide = most > kRowsMax;
+  p.rows = !p.wide || a.nseq > 1;
+  p.most_rows = kRowsMax;
+  p.wide_least = p.rows ? kRowsMax : 0;
+  size_t at = 256;  // the two kernels' split sizes
+  p.part_at = at;
+  if (p.rows) {
+    const long long m = std::min<long long>(most, kRowsMax);
+    p.row_blocks = blocks(m, kRowsMax);
+    p.target = keys <= kShortKeys ? 0 : kTarget;
+    p.rps = (int)m;
+    p.slots = (size_t)p.target + (size_t)p.row_blocks * a.heads;
+    if (p.target) at += up256(p.slots * p.rps * (dv + 1) * sizeof(float));
+  }
+  p.wide_at = at;
+  if (p.wide) {
+    p.wide_blocks = blocks(most, kWideRows);
+    p.split_wide = keys > kLeastTiles * kWideTile;
+    p.wide_rps = (int)std::min<long long>(most, kWideRows);
+    if (p.split_wide)
+      at += up256((size_t)kWideGroups * kWideRounds * p.wide_rps * (dv + 1) * sizeof(float));
+  }
+  p.ws_bytes = p.target || p.split_wide ? at : 0;
   return p;
 }
 
 hipError_t launch_paged_read(const PagedArgs& a, const PagedPlan& plan, int kv, int dk, int dv,
                              const void* q, long long qld, const float* beta, void* out, int H,
                              bool causal, bool obf16, void* ws, hipStream_t stream) {
-  ReadArgs r;
+  ReadArgs r = {};
   r.q = static_cast<const bf16*>(q);
   r.qld = qld;
   r.beta = beta;
   r.out = out;
-  r.part = static_cast<float*>(ws);
+  r.tps = static_cast<int*>(ws);
+  r.part = reinterpret_cast<float*>(static_cast<char*>(ws) + plan.part_at);
+  r.wide_part = reinterpret_cast<float*>(static_cast<char*>(ws) + plan.wide_at);
   r.H = H;
   r.G = H / a.heads;
   r.rps = plan.rps;
+  r.wide_rps = plan.wide_rps;
   r.target = plan.target;
+  r.split_wide = plan.split_wide;
+  r.most_rows = plan.most_rows;
+  r.wide_least = plan.wide_least;
   r.causal = causal;
   r.obf16 = obf16;
-  if (dk == 32 && dv == 32) return paged_rows<32, 32>(a, r, plan, kv, stream);
-  if (dk == 64 && dv == 64) return paged_rows<64, 64>(a, r, plan, kv, stream);
-  if (dk == 64 && dv == 32) return paged_rows<64, 32>(a, r, plan, kv, stream);
-  if (dk == 128 && dv == 128) return paged_rows<128, 128>(a, r, plan, kv, stream);
-  if (dk == 128 && dv == 64) return paged_rows<128, 64>(a, r, plan, kv, stream);
+  auto go = [&](auto rows, auto wide) {
+    hipError_t e = hipSuccess;
+    if (plan.wide) e = wide(a, r, plan, kv, stream);
+    if (e == hipSuccess && plan.rows) e = rows(a, r, plan, kv, stream);
+    return e;
+  };
+  if (dk == 32 && dv == 32) return go(paged_rows<32, 32>, paged_wide<32, 32>);
+  if (dk == 64 && dv == 64) return go(paged_rows<64, 64>, paged_wide<64, 64>);
+  if (dk == 64 && dv == 32) return go(paged_rows<64, 32>, paged_wide<64, 32>);
+  if (dk == 128 && dv == 128) return go(paged_rows<128, 128>, paged_wide<128, 128>);
+  if (dk == 128 && dv == 64) return go(paged_rows<128, 64>, paged_wide<128, 64>);
   return hipErrorInvalidValue;
 }
 

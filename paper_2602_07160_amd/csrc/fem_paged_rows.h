@@ -50,12 +50,21 @@ constexpr float kLoBelow = 0.5f;   // channels with beta below this take E as hi
 
 // ---- who does what ------------------------------------------------------------
 
-// The split of a call's work, formed by every wave from the lengths: sequence
-// b has nrb row blocks and nt key tiles; tps tiles make a split, so that all
-// splits of all heads number at most `target` + one a row block and head.
+// The part of a call that one kernel takes: the sequences with lo < rows <= hi
+// (rows: new tokens times query heads of a group), in row blocks of `br` rows and
+// key tiles of `tk` keys.
+struct Work {
+  int G, br, tk;
+  long long lo, hi;
+  int max_q;
+  bool causal;
+};
+
+// The split of the work, formed by every wave from the lengths: `tps` key tiles
+// make a split of a row block.
 struct RowItem {
   int b, rb, s, ns;  // sequence, row block, split and the number of splits
-  int slot;          // of split s of head 0 among the heads' slots
+  int slot;          // number of split s among those of one head
   Seq seq;
   bool found;
 };
@@ -64,11 +73,15 @@ struct RowCounts {
   int nrb, nt;
 };
 
-__device__ __forceinline__ RowCounts row_counts(const Seq& q, int G, int max_q) {
-  RowCounts c;
-  const bool ok = q.ok && q.n <= max_q;
-  c.nrb = (int)(((long long)q.n * G + kRowsMax - 1) / kRowsMax);
-  c.nt = ok ? max((q.len + kRowTile - 1) / kRowTile, 1) : 1;
+__device__ __forceinline__ RowCounts row_counts(const Seq& q, const Work& w) {
+  // a sequence that cannot be read is one item, whatever its rows (see all_nan)
+  const bool ok = q.ok && q.n <= w.max_q;
+  const long long rows = ok ? (long long)q.n * w.G : q.n > 0 ? 1 : 0;
+  RowCounts c = {0, 0};
+  if (rows > w.lo && rows <= w.hi) {
+    c.nrb = (int)((rows + w.br - 1) / w.br);
+    c.nt = ok ? max((q.len + w.tk - 1) / w.tk, 1) : 1;
+  }
   return c;
 }
 
@@ -77,27 +90,34 @@ __device__ __forceinline__ long long wave_sum64(long long x) {
   return x;
 }
 
-// Tiles of a split.
-__device__ __forceinline__ int tiles_per_split(const PagedArgs& a, int G, bool causal, int target) {
-  if (target == 0) return 1 << 30;  // one split each
+// Sum over the call's sequences of f(counts).
+template <class F>
+__device__ __forceinline__ long long sum_items(const PagedArgs& a, const Work& w, F&& f) {
   const int lane = threadIdx.x & 63;
   long long t = 0;
   for (int b0 = 0; b0 < a.nseq; b0 += 64) {
     const int b = b0 + lane;
-    if (b < a.nseq) {
-      const RowCounts c = row_counts(seq_of(a, b, causal), G, a.max_q);
-      t += (long long)c.nrb * c.nt;
-    }
+    if (b < a.nseq) t += f(row_counts(seq_of(a, b, w.causal), w));
   }
-  t = wave_sum64(t) * a.heads;
+  return wave_sum64(t);
+}
+
+constexpr int kWhole = 1 << 30;  // tiles of a split where nothing is split
+
+// Tiles of a split such that all splits of all heads number at most `target` + one
+// a row block and head.
+__device__ __forceinline__ int tiles_per_split(const PagedArgs& a, const Work& w, int target) {
+  if (target == 0) return kWhole;
+  const long long t =
+      sum_items(a, w, [](const RowCounts& c) { return (long long)c.nrb * c.nt; }) * a.heads;
   const long long tps = (t + target - 1) / target;
-  return (int)min(max(tps, (long long)kRowWaves), 1ll << 30);
+  return (int)min(max(tps, (long long)kRowWaves), (long long)kWhole);
 }
 
 // Item `x` of all heads' alike: a split of a row block (SPLITS), or a whole
 // row block.  Items are numbered by sequence, row block and split.
 template <bool SPLITS>
-__device__ __forceinline__ RowItem find_item(const PagedArgs& a, int G, bool causal, int tps, int x) {
+__device__ __forceinline__ RowItem find_item(const PagedArgs& a, const Work& w, int tps, int x) {
   const int lane = threadIdx.x & 63;
   RowItem it;
   it.found = false;
@@ -106,39 +126,37 @@ __device__ __forceinline__ RowItem find_item(const PagedArgs& a, int G, bool cau
     const int b = b0 + lane;
     int ns = 1, nrb = 0;
     if (b < a.nseq) {
-      const RowCounts c = row_counts(seq_of(a, b, causal), G, a.max_q);
+      const RowCounts c = row_counts(seq_of(a, b, w.causal), w);
       nrb = c.nrb;
-      ns = (c.nt + tps - 1) / tps;
+      ns = tps >= c.nt ? 1 : (c.nt + tps - 1) / tps;
     }
     const int mine = SPLITS ? nrb * ns : nrb, slots = nrb * ns;
     int end = mine, send = slots;
     for (int o = 1; o < 64; o <<= 1) {
-      const int u = __shfl_up(end, o), w = __shfl_up(send, o);
+      const int u = __shfl_up(end, o), v = __shfl_up(send, o);
       if (lane >= o) {
         end += u;
-        send += w;
+        send += v;
       }
     }
     const uint64_t m = __ballot(base + end > x);
     if (m != 0) {
       const int l = __builtin_ctzll(m);
       it.found = true;
-      it.b = b0 + l;
-      const int first = base + __shfl(end - mine, l);
-      it.ns = __shfl(ns, l);
-      const int at = x - first;
+      it.b = __builtin_amdgcn_readfirstlane(b0 + l);
+      const int at = __builtin_amdgcn_readfirstlane(x - base - __shfl(end - mine, l));
+      it.ns = __builtin_amdgcn_readfirstlane(__shfl(ns, l));
       it.rb = SPLITS ? at / it.ns : at;
       it.s = SPLITS ? at % it.ns : 0;
-      it.slot = slot + __shfl(send - slots, l) + it.rb * it.ns + it.s;
+      it.slot = __builtin_amdgcn_readfirstlane(slot + __shfl(send - slots, l)) + it.rb * it.ns + it.s;
       break;
     }
     base += __shfl(end, 63);
     slot += __shfl(send, 63);
   }
   if (it.found) {
-    it.b = __builtin_amdgcn_readfirstlane(it.b);
-    it.seq = seq_of(a, it.b, causal);
-    it.seq.ok = it.seq.ok && it.seq.n <= a.max_q;
+    it.seq = seq_of(a, it.b, w.causal);
+    it.seq.ok = it.seq.ok && it.seq.n <= w.max_q;
   }
   return it;
 }
@@ -455,12 +473,20 @@ struct ReadArgs {
   long long qld;
   const float* beta;   // [heads][DV]
   void* out;           // [ntok][H][DV] float32 or bf16
+  int* tps;            // [2] tiles of a split, as the two kernels have chosen them
   float* part;         // [slot][rps][DV + 1]: log2 joint sums, then the row's log2 normaliser
+  float* wide_part;    // of the wide kernel
   int H, G;            // query heads, of a cached head
-  int rps;             // rows of a slot
+  int rps, wide_rps;   // rows of a slot
   int target;          // see tiles_per_split
+  int split_wide;      // whether the wide kernel may split
+  long long most_rows, wide_least;  // the kernels' sequences: rows <= most, rows > least
   int causal, obf16;
 };
+
+__device__ __forceinline__ Work rows_work(const PagedArgs& a, const ReadArgs& r) {
+  return Work{r.G, kRowsMax, kRowTile, 0, r.most_rows, a.max_q, r.causal != 0};
+}
 
 __device__ __forceinline__ void put(const ReadArgs& r, size_t at, float x) {
   if (r.obf16) static_cast<bf16*>(r.out)[at] = (bf16)x;
@@ -496,7 +522,6 @@ __device__ __forceinline__ void rows_body(const PagedArgs& a, const ReadArgs& r,
     w.load_v(row);
   }
   int lim[RB];
-  int least = 0x7fffffff;  // keys that every row sees
 #pragma unroll
   for (int rb = 0; rb < RB; ++rb) {
     const int row = r0 + min(rb * 16 + w.l16, nr - 1);  // rows past the last repeat it
@@ -510,7 +535,7 @@ __device__ __forceinline__ void rows_body(const PagedArgs& a, const ReadArgs& r,
 #pragma unroll
     for (int cb = 0; cb < C::NCB; ++cb) w.acc[rb][cb] = f32x4{};
   }
-  least = row_limit(sq, r0, r.G, causal);
+  const int least = row_limit(sq, r0, r.G, causal);  // keys that every row sees
   w.lo_blocks = 0;
 #pragma unroll
   for (int cb = 0; cb < C::NCB; ++cb) {
@@ -620,6 +645,20 @@ __device__ __forceinline__ void rows_body(const PagedArgs& a, const ReadArgs& r,
   }
 }
 
+// The rows of an item that has nothing to read: all of its sequence's where the
+// sequence contradicts itself, the block's where it has no keys.
+template <int DV>
+__device__ __forceinline__ void all_nan(const ReadArgs& r, const RowItem& it, int g, int br,
+                                        int threads) {
+  const long long rows = (long long)it.seq.n * r.G;
+  const long long r0 = it.seq.ok ? (long long)it.rb * br : 0;
+  const long long r1 = it.seq.ok ? min(rows, r0 + br) : rows;
+  for (long long e = r0 * DV + threadIdx.x; e < r1 * DV; e += threads) {
+    const int row = (int)(e / DV);
+    put(r, ((size_t)(it.seq.q0 + row / r.G) * r.H + g * r.G + row % r.G) * DV + e % DV, NAN);
+  }
+}
+
 // Workgroup x * heads + g: item x of cached head g.
 template <int DK, int DV, int KV>
 __global__ __launch_bounds__(kRowThreads, 2) void paged_rows_kernel(PagedArgs a, ReadArgs r) {
@@ -627,37 +666,42 @@ __global__ __launch_bounds__(kRowThreads, 2) void paged_rows_kernel(PagedArgs a,
   __shared__ __align__(16) unsigned char
       smem[kRowWaves * C::AREA + kRowWaves * (2 * kRowsMax + DV) * 4 + 16];
   const int g = blockIdx.x % a.heads, x = blockIdx.x / a.heads;
-  const bool causal = r.causal != 0;
-  const int tps = tiles_per_split(a, r.G, causal, r.target);
-  const RowItem it = find_item<true>(a, r.G, causal, tps, x);
+  const Work wk = rows_work(a, r);
+  const int tps = tiles_per_split(a, wk, r.target);
+  if (r.target != 0 && blockIdx.x == 0 && threadIdx.x == 0) r.tps[0] = tps;
+  const RowItem it = find_item<true>(a, wk, tps, x);
   if (!it.found) return;
-  const int r0 = it.rb * kRowsMax, nr = min((int)min((long long)it.seq.n * r.G - r0, 32ll), 32);
-  if (!it.seq.ok || it.seq.len == 0) {  // nothing can be read, or there is nothing to read
-    for (int e = threadIdx.x; e < nr * DV; e += kRowThreads) {
-      const int row = r0 + e / DV;
-      put(r, ((size_t)(it.seq.q0 + row / r.G) * r.H + g * r.G + row % r.G) * DV + e % DV, NAN);
-    }
+  if (!it.seq.ok || it.seq.len == 0) {
+    all_nan<DV>(r, it, g, kRowsMax, kRowThreads);
     return;
   }
+  const int nr = (int)min((long long)it.seq.n * r.G - (long long)it.rb * kRowsMax, 32ll);
   if (nr <= 16) rows_body<DK, DV, KV, 1>(a, r, it, g, (int)blockIdx.x, smem);
   else rows_body<DK, DV, KV, 2>(a, r, it, g, (int)blockIdx.x, smem);
 }
 
-// Merge of the splits of row block x, cached head g.  The workgroup's threads
-// are groups of DV; few rows share the groups over the splits, many take a
-// group each.
+// Merge of the splits of row block x, cached head g, 32 rows a workgroup.  The
+// workgroup's threads are groups of DV; few rows share the groups over the splits,
+// many take a group each.
 constexpr int kMergeThreads = 512;
+constexpr int kMergeRows = 32;
 
 template <int DV>
-__global__ __launch_bounds__(kMergeThreads) void paged_merge_kernel(PagedArgs a, ReadArgs r) {
+__global__ __launch_bounds__(kMergeThreads) void paged_merge_kernel(PagedArgs a, ReadArgs r, Work w,
+                                                                    const int* tps_at,
+                                                                    const float* part, int rps) {
   constexpr int NG = kMergeThreads / DV;
-  __shared__ float4 part[NG][DV];
-  const int g = blockIdx.x % a.heads, x = blockIdx.x / a.heads;
-  const bool causal = r.causal != 0;
-  const int tps = tiles_per_split(a, r.G, causal, r.target);
-  const RowItem it = find_item<false>(a, r.G, causal, tps, x);
+  __shared__ float4 meet[NG][DV];
+  const int tps = *tps_at;
+  if (tps >= kWhole) return;
+  const int chunks = w.br / kMergeRows;
+  const int g = blockIdx.x % a.heads, xc = blockIdx.x / a.heads;
+  const RowItem it = find_item<false>(a, w, tps, xc / chunks);
   if (!it.found || it.ns == 1) return;
-  const int r0 = it.rb * kRowsMax, nr = min((int)min((long long)it.seq.n * r.G - r0, 32ll), 32);
+  const int c0 = xc % chunks * kMergeRows;  // first row of the block that is merged here
+  const int r0 = it.rb * w.br + c0;
+  const int nr = (int)min((long long)it.seq.n * r.G - r0, (long long)kMergeRows);
+  if (nr <= 0) return;
   int per = NG;  // groups of a row
   while (per > 1 && (NG / per) < nr) per >>= 1;
   const int rows = NG / per;  // rows at a time
@@ -682,16 +726,16 @@ __global__ __launch_bounds__(kMergeThreads) void paged_merge_kernel(PagedArgs a,
 #pragma unroll 4
       for (int s = sub; s < it.ns; s += per) {
         const float* p =
-            r.part + ((size_t)((size_t)(it.slot + s) * a.heads + g) * r.rps + q) * (DV + 1);
+            part + ((size_t)((size_t)(it.slot + s) * a.heads + g) * rps + c0 + q) * (DV + 1);
         join(M, S, p[j], one(p[j]));
         join(md, sd, p[DV], one(p[DV]));
       }
     }
-    part[grp][j] = make_float4(M, S, md, sd);
+    meet[grp][j] = make_float4(M, S, md, sd);
     __syncthreads();
     if (q < nr && sub == 0) {
       for (int u = 1; u < per; ++u) {
-        const float4 o = part[grp + u][j];
+        const float4 o = meet[grp + u][j];
         join(M, S, o.x, o.y);
         join(md, sd, o.z, o.w);
       }

@@ -1,10 +1,8 @@
-// Few-row paged reads at d_qk = 128 (fem_paged_rows.h).
+// Paged reads of few rows, d_qk = 128, d_v = 128.
 
 #include "fem_paged_launch.h"
 
 namespace fem {
-
 template hipError_t paged_rows<128, 128>(const PagedArgs&, const ReadArgs&, const PagedPlan&, int,
-                                         hipStream_t);
-
+                                     hipStream_t);
 }  // namespace fem

@@ -1,10 +1,8 @@
-// Few-row paged reads at d_qk = 32 (fem_paged_rows.h).
+// Paged reads of few rows, d_qk = 32, d_v = 32.
 
 #include "fem_paged_launch.h"
 
 namespace fem {
-
 template hipError_t paged_rows<32, 32>(const PagedArgs&, const ReadArgs&, const PagedPlan&, int,
-                                         hipStream_t);
-
+                                     hipStream_t);
 }  // namespace fem
