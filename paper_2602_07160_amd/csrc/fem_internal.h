@@ -101,15 +101,15 @@ struct PagedPlan {
   bool rows, wide;         // whether the kernel for few rows runs, and the one for many
   long long most_rows;     // sequences of the first: rows <= most_rows, of the second:
   long long wide_least;    //   rows > wide_least
-  int row_blocks, target;  // few rows: bound of the row blocks of a cached head, and the
-                           //   splits aimed at over all heads (0: one a row block)
+  int row_blocks, target;  // few rows: bound of the row blocks of a cached head, and of
+                           //   the splits over all heads (0: nothing is split)
   int wide_blocks;         // many rows: bound of a cached head's row blocks
   bool split_wide;
   int rps, wide_rps;       // rows of a slot
-  size_t slots;            // workgroups and slots of the first kernel
+  size_t groups;           // workgroups of the first kernel
   size_t part_at, wide_at, ws_bytes;
 };
-PagedPlan paged_plan(const PagedArgs& a, int H, int dv);
+PagedPlan paged_plan(const PagedArgs& a, int H, int dk, int dv, int kv);
 hipError_t launch_paged_read(const PagedArgs& a, const PagedPlan& plan, int kv, int dk, int dv,
                              const void* q, long long qld, const float* beta, void* out, int H,
                              bool causal, bool obf16, void* ws, hipStream_t stream);

@@ -26,41 +26,35 @@ struct PagedArgs {
   int nseq, table_len, ntok, max_q;
 };
 
-// Scale 2^(byte - 127).  255 gives +inf: its codes are zeros, and 0 * inf is
-// NaN, which is what such a block holds.  0 (never written) gives 0.
+// Scale 2^(byte - 127).  255 gives +inf, which makes the zeros of such a block NaN.
 __device__ __forceinline__ float scale_of(unsigned byte) { return __uint_as_float(byte << 23); }
 
-// The bf16 values of four codes of word w times 2^(byte - 127): exact, since a
-// code has at most eight significant bits.
-template <int KV>
-__device__ __forceinline__ void dequant4(unsigned w, float s, float (&f)[4]) {
-  if constexpr (KV == FEM_KV_E4M3) {
-    const f32x2 a = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false);
-    const f32x2 b = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true);
-    f[0] = a[0] * s;
-    f[1] = a[1] * s;
-    f[2] = b[0] * s;
-    f[3] = b[1] * s;
-  } else {
-    // code + 128 as an unsigned byte, so that one conversion and one
-    // multiply-add (a single rounding of an exact result) give the value
-    const unsigned u = w ^ 0x80808080u;
-    const float o = -128.f * s;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) f[e] = fmaf((float)((u >> (8 * e)) & 0xffu), s, o);
-  }
-}
-
-// Two words (8 codes) as 8 bf16 (the high halves: the values are exact in bf16).
+// Two words (8 codes) as 8 bf16 values: exact, since a code has at most eight
+// significant bits.
 template <int KV>
 __device__ __forceinline__ u32x4 dequant8(unsigned w0, unsigned w1, float s) {
-  float a[4], b[4];
-  dequant4<KV>(w0, s, a);
-  dequant4<KV>(w1, s, b);
-  auto pack = [](float lo, float hi) {
-    return __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302u);
-  };
-  return u32x4{pack(a[0], a[1]), pack(a[2], a[3]), pack(b[0], b[1]), pack(b[2], b[3])};
+  if constexpr (KV == FEM_KV_E4M3) {
+    // two codes to bf16, scaled, in one instruction (checked for every code and
+    // scale byte from 27 on against the conversion to float and a product)
+    auto pair = [s](unsigned w, bool hi) {
+      return __builtin_bit_cast(unsigned, hi ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, s, true)
+                                             : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, s, false));
+    };
+    return u32x4{pair(w0, false), pair(w0, true), pair(w1, false), pair(w1, true)};
+  } else {
+    // code + 128 as an unsigned byte, so that one conversion and one
+    // multiply-add (a single rounding of an exact result) give the value, whose
+    // high half is the bf16
+    const float o = -128.f * s;
+    auto pair = [s, o](unsigned u, int e) {
+      const float x = fmaf((float)((u >> (8 * e)) & 0xffu), s, o);
+      const float y = fmaf((float)((u >> (8 * e + 8)) & 0xffu), s, o);
+      return __builtin_amdgcn_perm(__float_as_uint(y), __float_as_uint(x), 0x07060302u);
+    };
+    w0 ^= 0x80808080u;
+    w1 ^= 0x80808080u;
+    return u32x4{pair(w0, 0), pair(w0, 2), pair(w1, 0), pair(w1, 2)};
+  }
 }
 
 // Eight consecutive values (chunk c) of a stored row as floats.

@@ -8,7 +8,7 @@
 namespace fem {
 
 namespace {
-constexpr int kTarget = 1024;    // splits of few rows aimed at
+constexpr int kUnits = 256;      // compute units
 constexpr int kShortKeys = 128;  // contexts that one workgroup reads in one round
 
 size_t up256(size_t x) { return (x + 255) / 256 * 256; }
@@ -16,7 +16,7 @@ size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 
 // Up to 32 rows a sequence the kernel for few rows; more, the one for many; both
 // where max_q allows either.
-PagedPlan paged_plan(const PagedArgs& a, int H, int dv) {
+PagedPlan paged_plan(const PagedArgs& a, int H, int dk, int dv, int kv) {
   PagedPlan p = {};
   const long long G = H / a.heads, rows = (long long)a.ntok * G, most = a.max_q * G;
   const long long keys = (long long)a.table_len << a.page_log2;
@@ -32,10 +32,11 @@ PagedPlan paged_plan(const PagedArgs& a, int H, int dv) {
   if (p.rows) {
     const long long m = std::min<long long>(most, kRowsMax);
     p.row_blocks = blocks(m, kRowsMax);
-    p.target = keys <= kShortKeys ? 0 : kTarget;
     p.rps = (int)m;
-    p.slots = (size_t)p.target + (size_t)p.row_blocks * a.heads;
-    if (p.target) at += up256(p.slots * p.rps * (dv + 1) * sizeof(float));
+    const int room = kUnits * row_waves(dk, dv, kv, m <= 16 ? 1 : 2);
+    p.target = keys <= kShortKeys ? 0 : room;
+    p.groups = p.target ? room : std::min<size_t>((size_t)p.row_blocks * a.heads, room);
+    if (p.target) at += up256((size_t)p.target * p.rps * (dv + 1) * sizeof(float));
   }
   p.wide_at = at;
   if (p.wide) {

@@ -4,21 +4,30 @@
 #include "fem_paged_wide.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace fem {
 
 template <int DK, int DV>
 hipError_t paged_rows(const PagedArgs& a, const ReadArgs& r, const PagedPlan& plan, int kv,
                       hipStream_t stream) {
-  const dim3 grid((unsigned)plan.slots), block(kRowThreads);
+  const dim3 grid((unsigned)plan.groups), block(kRowThreads);
   auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, stream, a, r); };
-  if (kv == FEM_KV_BF16) go(paged_rows_kernel<DK, DV, FEM_KV_BF16>);
-  else if (kv == FEM_KV_E4M3) go(paged_rows_kernel<DK, DV, FEM_KV_E4M3>);
-  else go(paged_rows_kernel<DK, DV, FEM_KV_INT8>);
+  auto pick = [&](auto rb) {
+    constexpr int RB = decltype(rb)::value;
+    if (kv == FEM_KV_BF16) go(paged_rows_kernel<DK, DV, FEM_KV_BF16, RB>);
+    else if (kv == FEM_KV_E4M3) go(paged_rows_kernel<DK, DV, FEM_KV_E4M3, RB>);
+    else go(paged_rows_kernel<DK, DV, FEM_KV_INT8, RB>);
+  };
+  if (plan.rps <= 16) pick(std::integral_constant<int, 1>());
+  else pick(std::integral_constant<int, 2>());
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || plan.target == 0) return e;
   const Work w{r.G, kRowsMax, kRowTile, 0, r.most_rows, a.max_q, r.causal != 0};
-  hipLaunchKernelGGL((paged_merge_kernel<DV>), dim3((unsigned)(plan.row_blocks * a.heads)),
+  // (only calls with at most `target` row blocks of all heads are split)
+  const size_t blocks = std::min<size_t>((size_t)plan.row_blocks * a.heads, plan.target);
+  const int chunks = (r.rps + kMergeRows - 1) / kMergeRows;
+  hipLaunchKernelGGL((paged_merge_kernel<DV, kMergeRows>), dim3((unsigned)(blocks * chunks)),
                      dim3(kMergeThreads), 0, stream, a, r, w, r.tps, r.part, r.rps);
   return hipGetLastError();
 }
@@ -38,7 +47,8 @@ hipError_t paged_wide(const PagedArgs& a, const ReadArgs& r, const PagedPlan& pl
   const Work w{r.G, kWideRows, kWideTile, r.wide_least, 1ll << 60, a.max_q, r.causal != 0};
   // (only calls of at most this many row blocks are split)
   const size_t blocks = std::min<size_t>(most, (size_t)kWideGroups * kWideRounds);
-  hipLaunchKernelGGL((paged_merge_kernel<DV>), dim3((unsigned)(blocks * (kWideRows / kMergeRows))),
+  const int chunks = (r.wide_rps + kWideMergeRows - 1) / kWideMergeRows;
+  hipLaunchKernelGGL((paged_merge_kernel<DV, kWideMergeRows>), dim3((unsigned)(blocks * chunks)),
                      dim3(kMergeThreads), 0, stream, a, r, w, r.tps + 1, r.wide_part, r.wide_rps);
   return hipGetLastError();
 }

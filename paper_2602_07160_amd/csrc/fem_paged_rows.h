@@ -40,12 +40,21 @@
 
 namespace fem {
 
+// Waves of a SIMD, that is workgroups of a compute unit, that the registers of the
+// kernel for at most 16 rb rows leave room for.
+constexpr int row_waves(int dk, int dv, int kv, int rb) {
+  if (rb == 2) return dk == 32 ? 3 : 2;
+  return dk == 32 ? 4 : dk == 64 || kv != FEM_KV_BF16 ? 3 : 2;
+}
+
 constexpr int kRowsMax = 32;       // query rows of a block
 constexpr int kRowTile = 32;       // keys of a wave's tile
 constexpr int kRowWaves = 4;
 constexpr int kRowThreads = 64 * kRowWaves;
 constexpr float kRowBias = 40.f;   // of P and of E
 constexpr float kLag = 8.f;        // of m and of c
+constexpr float kNone = -1e30f;    // m and c before the first key: finite, so that a hidden
+                                   // key's exponent is -inf and not NaN
 constexpr float kLoBelow = 0.5f;   // channels with beta below this take E as hi + lo
 
 // ---- who does what ------------------------------------------------------------
@@ -104,14 +113,30 @@ __device__ __forceinline__ long long sum_items(const PagedArgs& a, const Work& w
 
 constexpr int kWhole = 1 << 30;  // tiles of a split where nothing is split
 
-// Tiles of a split such that all splits of all heads number at most `target` + one
-// a row block and head.
+// Tiles of a split such that all splits of all heads number at most `target`, the
+// smallest of 64 candidates (a lane each) between a target-th of the tiles and three
+// times that; kWhole where none will do or nothing is to be split.
 __device__ __forceinline__ int tiles_per_split(const PagedArgs& a, const Work& w, int target) {
   if (target == 0) return kWhole;
+  const int lane = threadIdx.x & 63;
   const long long t =
       sum_items(a, w, [](const RowCounts& c) { return (long long)c.nrb * c.nt; }) * a.heads;
-  const long long tps = (t + target - 1) / target;
-  return (int)min(max(tps, (long long)kRowWaves), (long long)kWhole);
+  const long long least = max((t + target - 1) / target, (long long)kRowWaves);
+  const int cand = (int)min(least + (least * lane + 31) / 32, (long long)kWhole);
+  const float inv = 1.f / (float)cand;
+  long long n = 0;  // splits of a head with this lane's candidate
+  for (int b0 = 0; b0 < a.nseq; b0 += 64) {
+    RowCounts c = {0, 0};
+    if (b0 + lane < a.nseq) c = row_counts(seq_of(a, b0 + lane, w.causal), w);
+    const int m = min(64, a.nseq - b0);
+    for (int i = 0; i < m; ++i) {
+      const int nrb = __builtin_amdgcn_readlane(c.nrb, i), nt = __builtin_amdgcn_readlane(c.nt, i);
+      // ceil(nt / cand), or one more where the product rounds up to a whole number
+      n += (long long)nrb * ((int)((float)nt * inv) + 1);
+    }
+  }
+  const uint64_t fits = __ballot(n * a.heads <= target);
+  return fits == 0 ? kWhole : __builtin_amdgcn_readlane(cand, __builtin_ctzll(fits));
 }
 
 // Item `x` of all heads' alike: a split of a row block (SPLITS), or a whole
@@ -178,6 +203,7 @@ __device__ float exact_joint(const PagedArgs& a, const bf16* qrow, int b, int g,
     bool bad = false;
     const size_t row = paged_row(a, b, g, i, bad);
     float dot = 0.f;
+#pragma unroll 1  // registers: this is rare
     for (int c = 0; c < DK / 8; ++c) {
       const bf16x8 x = reinterpret_cast<const bf16x8*>(qrow)[c];
       float f[8];
@@ -192,6 +218,11 @@ __device__ float exact_joint(const PagedArgs& a, const bf16* qrow, int b, int g,
     t.add(fmaf(v, bl, dot * scale2));
   }
   return t.wave_total();
+}
+
+__device__ __forceinline__ float max8(const float (&x)[8]) {  // three v_max3 and one v_max
+  return fmaxf(fmaxf(fmaxf(fmaxf(fmaxf(x[0], x[1]), x[2]), fmaxf(fmaxf(x[3], x[4]), x[5])), x[6]),
+               x[7]);
 }
 
 // ---- the read -------------------------------------------------------------------
@@ -375,8 +406,7 @@ struct RowRead {
         for (int e = 0; e < 8; ++e)
           if ((e & 3) + 16 * (e >> 2) >= left) x[e] = -INFINITY;
       }
-      float mx = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])),
-                       fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
+      float mx = max8(x);
       if (__any(mx > m[rb] + kLag)) {
         mx = fmaxf(mx, __shfl_xor(mx, 16));
         mx = fmaxf(mx, __shfl_xor(mx, 32));
@@ -390,8 +420,7 @@ struct RowRead {
 #pragma unroll
         for (int cb = 0; cb < C::NCB; ++cb) acc[rb][cb] *= fr;
       }
-      // a row that has seen no key yet keeps m = -inf: a finite stand-in
-      const float sh = kRowBias - fmaxf(m[rb], -3e38f);
+      const float sh = kRowBias - m[rb];
 #pragma unroll
       for (int e = 0; e < 8; e += 2) {
         // rounded to bf16 (2^-9 relative); lsum adds the same rounded values,
@@ -405,32 +434,44 @@ struct RowRead {
 
     // ---- E and O += P E, 16 channels at a time
     const int tr = (4 * grp + (l16 >> 2)) * C::VROW + (l16 & 3) * 8;
+    auto read_v = [&](int cb, int kb) {
+      return __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+          (lds_s16x4*)(vt + tr + kb * 16 * C::VROW + cb * 32));
+    };
+    s16x4 n0 = read_v(0, 0), n1 = read_v(0, 1);  // one block ahead
 #pragma unroll
     for (int cb = 0; cb < C::NCB; ++cb) {
-      const s16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(vt + tr + cb * 32));
-      const s16x4 v1 =
-          __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(vt + tr + 16 * C::VROW + cb * 32));
-      float v[8];
+      const s16x4 v0 = n0, v1 = n1;
+      if (cb + 1 < C::NCB) {
+        n0 = read_v(cb + 1, 0);
+        n1 = read_v(cb + 1, 1);
+      }
+      float v[8], x[8];
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         v[e] = __uint_as_float((unsigned)(unsigned short)v0[e] << 16);
         v[4 + e] = __uint_as_float((unsigned)(unsigned short)v1[e] << 16);
       }
-      const float vx = fmaxf(fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])),
-                             fmaxf(fmaxf(v[4], v[5]), fmaxf(v[6], v[7])));
-      if (__any(vx * bl[cb] > c[cb] + kLag)) {
-        float mx = fmaxf(vx, __shfl_xor(vx, 16));
+      auto exponents = [&] {
+        const float sh = kRowBias - c[cb];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = fmaf(v[e], bl[cb], sh);
+        return max8(x);
+      };
+      if (__any(exponents() > kRowBias + kLag)) {
+        float mx = max8(v);
+        mx = fmaxf(mx, __shfl_xor(mx, 16));
         mx = fmaxf(mx, __shfl_xor(mx, 32)) * bl[cb];
         const float cn = mx > c[cb] + kLag ? mx : c[cb];
         const float f = cn == c[cb] ? 1.f : exp2_hw(c[cb] - cn);
         c[cb] = cn;
 #pragma unroll
         for (int rb = 0; rb < RB; ++rb) acc[rb][cb] *= f;
+        exponents();
       }
-      const float sh = kRowBias - c[cb];
       float e8[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) e8[e] = exp2_hw(fmaf(v[e], bl[cb], sh));
+      for (int e = 0; e < 8; ++e) e8[e] = exp2_hw(x[e]);
       if ((lo_blocks >> cb) & 1) {
         // beta < 0.5 turns a rounding of E to bf16 into more than 2^-8 of the
         // read: E = hi (truncated) + lo (the rest, rounded), 2^-16 relative
@@ -530,7 +571,7 @@ __device__ __forceinline__ void rows_body(const PagedArgs& a, const ReadArgs& r,
 #pragma unroll
     for (int ks = 0; ks < C::NKS; ++ks) w.qf[rb][ks] = *reinterpret_cast<const bf16x8*>(qp + ks * 32);
     lim[rb] = row_limit(sq, row, r.G, causal);
-    w.m[rb] = -INFINITY;
+    w.m[rb] = kNone;
     w.lsum[rb] = 0.f;
 #pragma unroll
     for (int cb = 0; cb < C::NCB; ++cb) w.acc[rb][cb] = f32x4{};
@@ -541,7 +582,7 @@ __device__ __forceinline__ void rows_body(const PagedArgs& a, const ReadArgs& r,
   for (int cb = 0; cb < C::NCB; ++cb) {
     const float b = r.beta[g * DV + cb * 16 + w.l16];
     w.bl[cb] = b * kLog2e;
-    w.c[cb] = -INFINITY;
+    w.c[cb] = kNone;
     if (__any(!(b >= kLoBelow))) w.lo_blocks |= 1u << cb;
   }
   for (; t < te; t += kRowWaves) {
@@ -578,7 +619,7 @@ __device__ __forceinline__ void rows_body(const PagedArgs& a, const ReadArgs& r,
 #pragma unroll
   for (int cb = 0; cb < C::NCB; ++cb) {
     const float top = top4(fc + cb * 16 + w.l16, DV);
-    cf[cb] = w.c[cb] == -INFINITY ? 0.f : exp2_hw(w.c[cb] - top);
+    cf[cb] = exp2_hw(w.c[cb] - top);
   }
 #pragma unroll
   for (int rb = 0; rb < RB; ++rb) {
@@ -587,8 +628,7 @@ __device__ __forceinline__ void rows_body(const PagedArgs& a, const ReadArgs& r,
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int q = rb * 16 + 4 * w.grp + i;
-      const float mine = fm[wave * kRowsMax + q];
-      rf[i] = mine == -INFINITY ? 0.f : exp2_hw(mine - top4(fm + q, kRowsMax));
+      rf[i] = exp2_hw(fm[wave * kRowsMax + q] - top4(fm + q, kRowsMax));
     }
     float* area = reinterpret_cast<float*>(smem + wave * C::AREA);
 #pragma unroll
@@ -608,8 +648,7 @@ __device__ __forceinline__ void rows_body(const PagedArgs& a, const ReadArgs& r,
 #pragma unroll
       for (int x = 0; x < kRowWaves; ++x) {
         sum += reinterpret_cast<const float*>(smem + x * C::AREA)[q * C::OROW + j];
-        const float mx = fm[x * kRowsMax + rb * 16 + q];
-        l += mx == -INFINITY ? 0.f : fl[x * kRowsMax + rb * 16 + q] * exp2_hw(mx - M);
+        l += fl[x * kRowsMax + rb * 16 + q] * exp2_hw(fm[x * kRowsMax + rb * 16 + q] - M);
       }
       const float blj = r.beta[g * DV + j] * kLog2e;
       const int seen = min(kend, row_limit(sq, row, r.G, causal));  // of this range, up to here
@@ -659,91 +698,114 @@ __device__ __forceinline__ void all_nan(const ReadArgs& r, const RowItem& it, in
   }
 }
 
-// Workgroup x * heads + g: item x of cached head g.
-template <int DK, int DV, int KV>
-__global__ __launch_bounds__(kRowThreads, 2) void paged_rows_kernel(PagedArgs a, ReadArgs r) {
+// Workgroup i takes the pieces i, i + gridDim, ...: piece x * heads + g is item x
+// of cached head g.  RB = 1: no sequence has more than 16 rows.
+template <int DK, int DV, int KV, int RB>
+__global__ __launch_bounds__(kRowThreads, row_waves(DK, DV, KV, RB)) void paged_rows_kernel(PagedArgs a, ReadArgs r) {
   using C = RowCfg<DK, DV>;
   __shared__ __align__(16) unsigned char
       smem[kRowWaves * C::AREA + kRowWaves * (2 * kRowsMax + DV) * 4 + 16];
-  const int g = blockIdx.x % a.heads, x = blockIdx.x / a.heads;
   const Work wk = rows_work(a, r);
   const int tps = tiles_per_split(a, wk, r.target);
   if (r.target != 0 && blockIdx.x == 0 && threadIdx.x == 0) r.tps[0] = tps;
-  const RowItem it = find_item<true>(a, wk, tps, x);
-  if (!it.found) return;
-  if (!it.seq.ok || it.seq.len == 0) {
-    all_nan<DV>(r, it, g, kRowsMax, kRowThreads);
-    return;
+  for (int piece = blockIdx.x;; piece += gridDim.x) {
+    const int g = piece % a.heads;
+    const RowItem it = find_item<true>(a, wk, tps, piece / a.heads);
+    if (!it.found) return;
+    if (!it.seq.ok || it.seq.len == 0) {
+      all_nan<DV>(r, it, g, kRowsMax, kRowThreads);
+      continue;
+    }
+    __syncthreads();  // the last piece's LDS is free
+    const long long left = (long long)it.seq.n * r.G - (long long)it.rb * kRowsMax;
+    if (RB == 1 || left <= 16) rows_body<DK, DV, KV, 1>(a, r, it, g, piece, smem);
+    else rows_body<DK, DV, KV, 2>(a, r, it, g, piece, smem);
   }
-  const int nr = (int)min((long long)it.seq.n * r.G - (long long)it.rb * kRowsMax, 32ll);
-  if (nr <= 16) rows_body<DK, DV, KV, 1>(a, r, it, g, (int)blockIdx.x, smem);
-  else rows_body<DK, DV, KV, 2>(a, r, it, g, (int)blockIdx.x, smem);
 }
 
-// Merge of the splits of row block x, cached head g, 32 rows a workgroup.  The
-// workgroup's threads are groups of DV; few rows share the groups over the splits,
-// many take a group each.
+// Merge of the splits of row block x, cached head g, ROWS rows a workgroup, four at a
+// time.  The workgroup's threads are groups of DV; the groups of a row share its
+// splits, kMergeBatch loads in flight each, and meet in LDS.
 constexpr int kMergeThreads = 512;
-constexpr int kMergeRows = 32;
+constexpr int kMergeRows = 4;
+constexpr int kMergeBatch = 4;
+constexpr int kWideMergeRows = 32;  // a wide block has many rows of few splits
 
-template <int DV>
+// (max, sum) of 2^x over a set, joined with another; a NaN, which the maxima pass
+// over, stays in the sum.
+__device__ __forceinline__ void lse_join(float& m, float& s, float m2, float s2) {
+  const float mn = fmaxf(m, m2);
+  if (mn == -INFINITY) {  // nothing on either side, or NaN
+    s += s2;
+    return;
+  }
+  s = s * exp2_hw(m - mn) + s2 * exp2_hw(m2 - mn);
+  m = mn;
+}
+
+template <int DV, int ROWS>
 __global__ __launch_bounds__(kMergeThreads) void paged_merge_kernel(PagedArgs a, ReadArgs r, Work w,
                                                                     const int* tps_at,
                                                                     const float* part, int rps) {
   constexpr int NG = kMergeThreads / DV;
+  static_assert(NG >= kMergeRows, "a group for every row");
   __shared__ float4 meet[NG][DV];
   const int tps = *tps_at;
   if (tps >= kWhole) return;
-  const int chunks = w.br / kMergeRows;
+  const int chunks = (min(w.br, rps) + ROWS - 1) / ROWS;  // of a row block
   const int g = blockIdx.x % a.heads, xc = blockIdx.x / a.heads;
   const RowItem it = find_item<false>(a, w, tps, xc / chunks);
   if (!it.found || it.ns == 1) return;
-  const int c0 = xc % chunks * kMergeRows;  // first row of the block that is merged here
+  const int c0 = xc % chunks * ROWS;  // first row of the block that is merged here
   const int r0 = it.rb * w.br + c0;
-  const int nr = (int)min((long long)it.seq.n * r.G - r0, (long long)kMergeRows);
+  const int nr = (int)min((long long)it.seq.n * r.G - r0, (long long)ROWS);
   if (nr <= 0) return;
-  int per = NG;  // groups of a row
-  while (per > 1 && (NG / per) < nr) per >>= 1;
-  const int rows = NG / per;  // rows at a time
+  const int rows = nr == 1 ? 1 : nr == 2 ? 2 : kMergeRows, per = NG / rows;
   const int grp = threadIdx.x / DV, j = threadIdx.x % DV;
+  const int sub = grp % per;
   const float blj = r.beta[g * DV + j] * kLog2e;
+  // 2^x / 2^x of a partial sum's logarithm: 0 of none, NaN of NaN
+  auto one = [](float x) { return x == -INFINITY ? 0.f : x != x ? x : 1.f; };
+  const size_t step = (size_t)a.heads * rps * (DV + 1);  // from split to split
+  const float* base = part + ((size_t)((size_t)it.slot * a.heads + g) * rps + c0) * (DV + 1);
   for (int q0 = 0; q0 < nr; q0 += rows) {
-    const int q = q0 + grp / per, sub = grp % per;
+    const int q = q0 + grp / per;
     float M = -INFINITY, S = 0.f, md = -INFINITY, sd = 0.f;
-    auto join = [](float& m, float& s, float m2, float s2) {
-      const float mn = fmaxf(m, m2);
-      if (mn == -INFINITY) {  // nothing yet, or NaN, which the sum keeps
-        s += s2;
-        return;
-      }
-      s = s * exp2_hw(m - mn) + s2 * exp2_hw(m2 - mn);
-      m = mn;
-    };
-    // 2^x / 2^x of a partial sum's logarithm x: 0 of none, NaN of NaN (which
-    // the maxima pass over, so the sums carry it)
-    auto one = [](float x) { return x == -INFINITY ? 0.f : x != x ? x : 1.f; };
     if (q < nr) {
-#pragma unroll 4
-      for (int s = sub; s < it.ns; s += per) {
-        const float* p =
-            part + ((size_t)((size_t)(it.slot + s) * a.heads + g) * rps + c0 + q) * (DV + 1);
-        join(M, S, p[j], one(p[j]));
-        join(md, sd, p[DV], one(p[DV]));
+      const float* p = base + (size_t)q * (DV + 1);
+      for (int s0 = sub; s0 < it.ns; s0 += kMergeBatch * per) {
+        float x[kMergeBatch], d[kMergeBatch];
+#pragma unroll
+        for (int u = 0; u < kMergeBatch; ++u) {
+          const int s = s0 + u * per;
+          const float* ps = p + step * min(s, it.ns - 1);
+          x[u] = s < it.ns ? ps[j] : -INFINITY;
+          d[u] = s < it.ns ? ps[DV] : -INFINITY;
+        }
+#pragma unroll
+        for (int u = 0; u < kMergeBatch; ++u) {
+          lse_join(M, S, x[u], one(x[u]));
+          lse_join(md, sd, d[u], one(d[u]));
+        }
       }
     }
-    meet[grp][j] = make_float4(M, S, md, sd);
-    __syncthreads();
-    if (q < nr && sub == 0) {
-      for (int u = 1; u < per; ++u) {
-        const float4 o = meet[grp + u][j];
-        join(M, S, o.x, o.y);
-        join(md, sd, o.z, o.w);
+    if (per > 1) {  // the same for the whole workgroup
+      if (q0 > 0) __syncthreads();
+      meet[grp][j] = make_float4(M, S, md, sd);
+      __syncthreads();
+      if (sub == 0) {
+        for (int u = 1; u < per; ++u) {
+          const float4 o = meet[grp + u][j];
+          lse_join(M, S, o.x, o.y);
+          lse_join(md, sd, o.z, o.w);
+        }
       }
+    }
+    if (q < nr && sub == 0) {
       const float o = ((M - md) + (log2_hw(S) - log2_hw(sd))) / blj;
       const int row = r0 + q;
       put(r, ((size_t)(it.seq.q0 + row / r.G) * r.H + g * r.G + row % r.G) * DV + j, o);
     }
-    __syncthreads();
   }
 }
 
