@@ -106,7 +106,7 @@ struct PagedPlan {
   int wide_blocks;         // many rows: bound of a cached head's row blocks
   bool split_wide;
   int rps, wide_rps;       // rows of a slot
-  size_t groups;           // workgroups of the first kernel
+  size_t groups, wide_groups;  // workgroups
   size_t part_at, wide_at, ws_bytes;
 };
 PagedPlan paged_plan(const PagedArgs& a, int H, int dk, int dv, int kv);

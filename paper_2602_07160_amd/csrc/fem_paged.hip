@@ -9,7 +9,8 @@ namespace fem {
 
 namespace {
 constexpr int kUnits = 256;      // compute units
-constexpr int kShortKeys = 128;  // contexts that one workgroup reads in one round
+constexpr int kShortKeys = 512;  // contexts that are not split: four tiles a wave
+constexpr int kMergeRows = 4, kWideMergeRows = 16;  // of a merge's workgroup
 
 size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 }  // namespace
@@ -43,8 +44,11 @@ PagedPlan paged_plan(const PagedArgs& a, int H, int dk, int dv, int kv) {
     p.wide_blocks = blocks(most, kWideRows);
     p.split_wide = keys > kLeastTiles * kWideTile;
     p.wide_rps = (int)std::min<long long>(most, kWideRows);
-    if (p.split_wide)
-      at += up256((size_t)kWideGroups * kWideRounds * p.wide_rps * (dv + 1) * sizeof(float));
+    p.wide_groups = (size_t)p.wide_blocks * a.heads;
+    if (p.split_wide) {
+      p.wide_groups = std::max<size_t>(p.wide_groups, kWideUnits);
+      at += up256((size_t)kWideUnits * p.wide_rps * (dv + 1) * sizeof(float));
+    }
   }
   p.ws_bytes = p.target || p.split_wide ? at : 0;
   return p;
@@ -71,17 +75,37 @@ hipError_t launch_paged_read(const PagedArgs& a, const PagedPlan& plan, int kv, 
   r.wide_least = plan.wide_least;
   r.causal = causal;
   r.obf16 = obf16;
-  auto go = [&](auto rows, auto wide) {
+  // A merge's workgroups.  Splits number at most `target` (few rows) or one a
+  // compute unit, and a block that is split has two at least.
+  MergePart few = {}, many = {};
+  if (plan.rows && plan.target) {
+    few = MergePart{rows_work(a, r), r.tps, r.part, plan.rps, kMergeRows, 0};
+    const size_t blocks = std::min<size_t>((size_t)plan.row_blocks * a.heads, plan.target);
+    few.groups = (int)(blocks * ((plan.rps + kMergeRows - 1) / kMergeRows));
+  }
+  if (plan.wide && plan.split_wide) {
+    many = MergePart{wide_work(a, r), r.tps + 1, r.wide_part, plan.wide_rps, kWideMergeRows, 0};
+    const size_t blocks = std::min<size_t>((size_t)plan.wide_blocks * a.heads, kWideUnits);
+    many.groups = (int)(blocks * ((plan.wide_rps + kWideMergeRows - 1) / kWideMergeRows));
+  }
+  auto go = [&](auto rows, auto wide, auto merge) {
     hipError_t e = hipSuccess;
     if (plan.wide) e = wide(a, r, plan, kv, stream);
     if (e == hipSuccess && plan.rows) e = rows(a, r, plan, kv, stream);
+    if (e == hipSuccess && few.groups + many.groups > 0) {
+      hipLaunchKernelGGL(merge, dim3((unsigned)(few.groups + many.groups)), dim3(kMergeThreads), 0,
+                         stream, a, r, few, many);
+      e = hipGetLastError();
+    }
     return e;
   };
-  if (dk == 32 && dv == 32) return go(paged_rows<32, 32>, paged_wide<32, 32>);
-  if (dk == 64 && dv == 64) return go(paged_rows<64, 64>, paged_wide<64, 64>);
-  if (dk == 64 && dv == 32) return go(paged_rows<64, 32>, paged_wide<64, 32>);
-  if (dk == 128 && dv == 128) return go(paged_rows<128, 128>, paged_wide<128, 128>);
-  if (dk == 128 && dv == 64) return go(paged_rows<128, 64>, paged_wide<128, 64>);
+  if (dk == 32 && dv == 32) return go(paged_rows<32, 32>, paged_wide<32, 32>, paged_merge_kernel<32>);
+  if (dk == 64 && dv == 64) return go(paged_rows<64, 64>, paged_wide<64, 64>, paged_merge_kernel<64>);
+  if (dk == 64 && dv == 32) return go(paged_rows<64, 32>, paged_wide<64, 32>, paged_merge_kernel<32>);
+  if (dk == 128 && dv == 128)
+    return go(paged_rows<128, 128>, paged_wide<128, 128>, paged_merge_kernel<128>);
+  if (dk == 128 && dv == 64)
+    return go(paged_rows<128, 64>, paged_wide<128, 64>, paged_merge_kernel<64>);
   return hipErrorInvalidValue;
 }
 

@@ -67,6 +67,7 @@ struct Work {
   long long lo, hi;
   int max_q;
   bool causal;
+  bool longest_first;  // items in the order of falling lengths (up to 64 sequences)
 };
 
 // The split of the work, formed by every wave from the lengths: `tps` key tiles
@@ -94,12 +95,7 @@ __device__ __forceinline__ RowCounts row_counts(const Seq& q, const Work& w) {
   return c;
 }
 
-__device__ __forceinline__ long long wave_sum64(long long x) {
-  for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o);
-  return x;
-}
-
-// Sum over the call's sequences of f(counts).
+// Sum over the call's sequences of f(counts), the same in every lane.
 template <class F>
 __device__ __forceinline__ long long sum_items(const PagedArgs& a, const Work& w, F&& f) {
   const int lane = threadIdx.x & 63;
@@ -108,7 +104,10 @@ __device__ __forceinline__ long long sum_items(const PagedArgs& a, const Work& w
     const int b = b0 + lane;
     if (b < a.nseq) t += f(row_counts(seq_of(a, b, w.causal), w));
   }
-  return wave_sum64(t);
+  const int m = min(64, a.nseq);  // lanes with a sequence
+  for (int o = 1; o < m; o <<= 1) t += __shfl_xor(t, o);
+  return (long long)(unsigned)__builtin_amdgcn_readfirstlane((int)t) |
+         (long long)__builtin_amdgcn_readfirstlane((int)(t >> 32)) << 32;
 }
 
 constexpr int kWhole = 1 << 30;  // tiles of a split where nothing is split
@@ -139,8 +138,9 @@ __device__ __forceinline__ int tiles_per_split(const PagedArgs& a, const Work& w
   return fits == 0 ? kWhole : __builtin_amdgcn_readlane(cand, __builtin_ctzll(fits));
 }
 
-// Item `x` of all heads' alike: a split of a row block (SPLITS), or a whole
-// row block.  Items are numbered by sequence, row block and split.
+// Item `x` of all heads' alike: a split of a row block (SPLITS), or a whole row
+// block.  Items are numbered by sequence, row block and split; longest_first takes
+// the sequences by length and a sequence's last row block first.
 template <bool SPLITS>
 __device__ __forceinline__ RowItem find_item(const PagedArgs& a, const Work& w, int tps, int x) {
   const int lane = threadIdx.x & 63;
@@ -149,35 +149,48 @@ __device__ __forceinline__ RowItem find_item(const PagedArgs& a, const Work& w, 
   int base = 0, slot = 0;
   for (int b0 = 0; b0 < a.nseq; b0 += 64) {
     const int b = b0 + lane;
-    int ns = 1, nrb = 0;
-    if (b < a.nseq) {
-      const RowCounts c = row_counts(seq_of(a, b, w.causal), w);
-      nrb = c.nrb;
-      ns = tps >= c.nt ? 1 : (c.nt + tps - 1) / tps;
+    RowCounts c = {0, 0};
+    if (b < a.nseq) c = row_counts(seq_of(a, b, w.causal), w);
+    const int m64 = min(64, a.nseq - b0);
+    int who = b;  // this lane's sequence
+    if (w.longest_first && a.nseq <= 64) {
+      int rank = lane;
+      if (lane < m64) {
+        rank = 0;
+        for (int i = 0; i < m64; ++i) {
+          const int t = __builtin_amdgcn_readlane(c.nt, i);
+          rank += t > c.nt || (t == c.nt && i < lane);
+        }
+      }
+      who = __builtin_amdgcn_ds_permute(rank * 4, who);
+      c.nt = __builtin_amdgcn_ds_permute(rank * 4, c.nt);
+      c.nrb = __builtin_amdgcn_ds_permute(rank * 4, c.nrb);
     }
+    const int nrb = c.nrb, ns = tps >= c.nt ? 1 : (c.nt + tps - 1) / tps;
     const int mine = SPLITS ? nrb * ns : nrb, slots = nrb * ns;
     int end = mine, send = slots;
-    for (int o = 1; o < 64; o <<= 1) {
-      const int u = __shfl_up(end, o), v = __shfl_up(send, o);
+    for (int o = 1; o < m64; o <<= 1) {
+      const int u = __shfl_up(end, o), v = SPLITS ? u : __shfl_up(send, o);
       if (lane >= o) {
         end += u;
         send += v;
       }
     }
-    const uint64_t m = __ballot(base + end > x);
+    const uint64_t m = __ballot(lane < m64 && base + end > x);
     if (m != 0) {
       const int l = __builtin_ctzll(m);
       it.found = true;
-      it.b = __builtin_amdgcn_readfirstlane(b0 + l);
+      it.b = __builtin_amdgcn_readlane(who, l);
       const int at = __builtin_amdgcn_readfirstlane(x - base - __shfl(end - mine, l));
       it.ns = __builtin_amdgcn_readfirstlane(__shfl(ns, l));
-      it.rb = SPLITS ? at / it.ns : at;
+      const int block = SPLITS ? at / it.ns : at;
       it.s = SPLITS ? at % it.ns : 0;
-      it.slot = __builtin_amdgcn_readfirstlane(slot + __shfl(send - slots, l)) + it.rb * it.ns + it.s;
+      it.slot = __builtin_amdgcn_readfirstlane(slot + __shfl(send - slots, l)) + block * it.ns + it.s;
+      it.rb = w.longest_first ? __builtin_amdgcn_readlane(nrb, l) - 1 - block : block;
       break;
     }
-    base += __shfl(end, 63);
-    slot += __shfl(send, 63);
+    base += __shfl(end, m64 - 1);
+    slot += __shfl(send, m64 - 1);
   }
   if (it.found) {
     it.seq = seq_of(a, it.b, w.causal);
@@ -525,8 +538,8 @@ struct ReadArgs {
   int causal, obf16;
 };
 
-__device__ __forceinline__ Work rows_work(const PagedArgs& a, const ReadArgs& r) {
-  return Work{r.G, kRowsMax, kRowTile, 0, r.most_rows, a.max_q, r.causal != 0};
+__host__ __device__ __forceinline__ Work rows_work(const PagedArgs& a, const ReadArgs& r) {
+  return Work{r.G, kRowsMax, kRowTile, 0, r.most_rows, a.max_q, r.causal != 0, false};
 }
 
 __device__ __forceinline__ void put(const ReadArgs& r, size_t at, float x) {
@@ -723,13 +736,7 @@ __global__ __launch_bounds__(kRowThreads, row_waves(DK, DV, KV, RB)) void paged_
   }
 }
 
-// Merge of the splits of row block x, cached head g, ROWS rows a workgroup, four at a
-// time.  The workgroup's threads are groups of DV; the groups of a row share its
-// splits, kMergeBatch loads in flight each, and meet in LDS.
-constexpr int kMergeThreads = 512;
-constexpr int kMergeRows = 4;
-constexpr int kMergeBatch = 4;
-constexpr int kWideMergeRows = 32;  // a wide block has many rows of few splits
+// ---- merge of the splits -------------------------------------------------------
 
 // (max, sum) of 2^x over a set, joined with another; a NaN, which the maxima pass
 // over, stays in the sum.
@@ -743,48 +750,64 @@ __device__ __forceinline__ void lse_join(float& m, float& s, float m2, float s2)
   m = mn;
 }
 
-template <int DV, int ROWS>
-__global__ __launch_bounds__(kMergeThreads) void paged_merge_kernel(PagedArgs a, ReadArgs r, Work w,
-                                                                    const int* tps_at,
-                                                                    const float* part, int rps) {
+// One of the two kernels' partial results, in chunks of `rows` rows of a row block.
+struct MergePart {
+  Work w;
+  const int* tps;
+  const float* part;
+  int rps, rows, groups;  // rows of a slot, of a chunk; workgroups
+};
+
+constexpr int kMergeThreads = 512;
+constexpr int kMergeBatch = 4;
+
+// Workgroup (chunk of a row block, cached head); the first p.groups of them for p,
+// the others for o.  The threads are groups of DV; a row's splits are shared by so
+// many groups (a power of two) that each takes one batch of them, if there are
+// enough, and the groups meet in LDS.
+template <int DV>
+__global__ __launch_bounds__(kMergeThreads) void paged_merge_kernel(PagedArgs a, ReadArgs r,
+                                                                    MergePart p, MergePart o) {
   constexpr int NG = kMergeThreads / DV;
-  static_assert(NG >= kMergeRows, "a group for every row");
   __shared__ float4 meet[NG][DV];
-  const int tps = *tps_at;
+  const bool second = (int)blockIdx.x >= p.groups;
+  const MergePart& x = second ? o : p;
+  const int tps = *x.tps;
   if (tps >= kWhole) return;
-  const int chunks = (min(w.br, rps) + ROWS - 1) / ROWS;  // of a row block
-  const int g = blockIdx.x % a.heads, xc = blockIdx.x / a.heads;
-  const RowItem it = find_item<false>(a, w, tps, xc / chunks);
+  const int id = second ? blockIdx.x - p.groups : blockIdx.x;
+  const int chunks = (min(x.w.br, x.rps) + x.rows - 1) / x.rows;  // of a row block
+  const int g = id % a.heads, xc = id / a.heads;
+  const RowItem it = find_item<false>(a, x.w, tps, xc / chunks);
   if (!it.found || it.ns == 1) return;
-  const int c0 = xc % chunks * ROWS;  // first row of the block that is merged here
-  const int r0 = it.rb * w.br + c0;
-  const int nr = (int)min((long long)it.seq.n * r.G - r0, (long long)ROWS);
+  const int c0 = xc % chunks * x.rows;  // first row of the block that is merged here
+  const int r0 = it.rb * x.w.br + c0;
+  const int nr = (int)min((long long)it.seq.n * r.G - r0, (long long)x.rows);
   if (nr <= 0) return;
-  const int rows = nr == 1 ? 1 : nr == 2 ? 2 : kMergeRows, per = NG / rows;
-  const int grp = threadIdx.x / DV, j = threadIdx.x % DV;
-  const int sub = grp % per;
+  int per = 1;  // groups of a row
+  while (per < NG && (per * kMergeBatch < it.ns || NG / per > nr)) per <<= 1;
+  const int rows = NG / per, grp = threadIdx.x / DV, j = threadIdx.x % DV, sub = grp % per;
   const float blj = r.beta[g * DV + j] * kLog2e;
   // 2^x / 2^x of a partial sum's logarithm: 0 of none, NaN of NaN
-  auto one = [](float x) { return x == -INFINITY ? 0.f : x != x ? x : 1.f; };
-  const size_t step = (size_t)a.heads * rps * (DV + 1);  // from split to split
-  const float* base = part + ((size_t)((size_t)it.slot * a.heads + g) * rps + c0) * (DV + 1);
+  auto one = [](float y) { return y == -INFINITY ? 0.f : y != y ? y : 1.f; };
+  const size_t step = (size_t)a.heads * x.rps * (DV + 1);  // from split to split
+  const float* base = x.part + ((size_t)((size_t)it.slot * a.heads + g) * x.rps + c0) * (DV + 1);
   for (int q0 = 0; q0 < nr; q0 += rows) {
     const int q = q0 + grp / per;
     float M = -INFINITY, S = 0.f, md = -INFINITY, sd = 0.f;
     if (q < nr) {
-      const float* p = base + (size_t)q * (DV + 1);
+      const float* pq = base + (size_t)q * (DV + 1);
       for (int s0 = sub; s0 < it.ns; s0 += kMergeBatch * per) {
-        float x[kMergeBatch], d[kMergeBatch];
+        float y[kMergeBatch], d[kMergeBatch];
 #pragma unroll
         for (int u = 0; u < kMergeBatch; ++u) {
           const int s = s0 + u * per;
-          const float* ps = p + step * min(s, it.ns - 1);
-          x[u] = s < it.ns ? ps[j] : -INFINITY;
+          const float* ps = pq + step * min(s, it.ns - 1);
+          y[u] = s < it.ns ? ps[j] : -INFINITY;
           d[u] = s < it.ns ? ps[DV] : -INFINITY;
         }
 #pragma unroll
         for (int u = 0; u < kMergeBatch; ++u) {
-          lse_join(M, S, x[u], one(x[u]));
+          lse_join(M, S, y[u], one(y[u]));
           lse_join(md, sd, d[u], one(d[u]));
         }
       }
@@ -795,16 +818,16 @@ __global__ __launch_bounds__(kMergeThreads) void paged_merge_kernel(PagedArgs a,
       __syncthreads();
       if (sub == 0) {
         for (int u = 1; u < per; ++u) {
-          const float4 o = meet[grp + u][j];
-          lse_join(M, S, o.x, o.y);
-          lse_join(md, sd, o.z, o.w);
+          const float4 z = meet[grp + u][j];
+          lse_join(M, S, z.x, z.y);
+          lse_join(md, sd, z.z, z.w);
         }
       }
     }
     if (q < nr && sub == 0) {
-      const float o = ((M - md) + (log2_hw(S) - log2_hw(sd))) / blj;
+      const float f = ((M - md) + (log2_hw(S) - log2_hw(sd))) / blj;
       const int row = r0 + q;
-      put(r, ((size_t)(it.seq.q0 + row / r.G) * r.H + g * r.G + row % r.G) * DV + j, o);
+      put(r, ((size_t)(it.seq.q0 + row / r.G) * r.H + g * r.G + row % r.G) * DV + j, f);
     }
   }
 }

@@ -484,18 +484,17 @@ __device__ __forceinline__ void wide_nlo(int nlo, const PagedArgs& a, const Read
   }
 }
 
-__device__ __forceinline__ Work wide_work(const PagedArgs& a, const ReadArgs& r) {
-  return Work{r.G, kWideRows, kWideTile, r.wide_least, 1ll << 60, a.max_q, r.causal != 0};
+__host__ __device__ __forceinline__ Work wide_work(const PagedArgs& a, const ReadArgs& r) {
+  return Work{r.G, kWideRows, kWideTile, r.wide_least, 1ll << 60, a.max_q, r.causal != 0, true};
 }
 
-constexpr int kWideGroups = 256;   // workgroups at a time: one a compute unit
-constexpr int kWideRounds = 2;     // splits number at most this many times that
-constexpr int kSplitCost = 5;      // a split's store and merge, in tiles
-constexpr int kLeastTiles = 4;     // of a split
+constexpr int kWideUnits = 256;  // compute units, which hold one workgroup each
+constexpr int kSplitCost = 8;    // a split's store and its part of the merge, in tiles
+constexpr int kLeastTiles = 4;   // of a split
 
-// Tiles of a split of the wide kernel: where the row blocks leave compute units
-// idle, the smallest split with which all splits fit one or two rounds, if the
-// rounds then take fewer tiles than whole blocks.
+// Tiles of a split of the wide kernel.  Where the row blocks leave at least half of
+// the compute units idle, the smallest with which all splits still have a unit each,
+// if that saves more tiles than the splits cost.
 __device__ __forceinline__ int wide_tiles(const PagedArgs& a, const ReadArgs& r, const Work& w) {
   if (!r.split_wide) return kWhole;
   const auto count = [&](int tps) {
@@ -504,35 +503,25 @@ __device__ __forceinline__ int wide_tiles(const PagedArgs& a, const ReadArgs& r,
            }) * a.heads;
   };
   const long long items = count(kWhole);
-  if (items == 0 || items > kWideGroups * kWideRounds) return kWhole;
+  if (items == 0 || items * 2 > kWideUnits) return kWhole;
   int longest = 0;
   for (int b0 = 0; b0 < a.nseq; b0 += 64) {
     const int b = b0 + (threadIdx.x & 63);
     if (b < a.nseq) longest = max(longest, row_counts(seq_of(a, b, w.causal), w).nt);
   }
   for (int o = 32; o > 0; o >>= 1) longest = max(longest, __shfl_xor(longest, o));
-  int best = kWhole;
-  long long span = (items + kWideGroups - 1) / kWideGroups * longest;
-  for (int rounds = 1; rounds <= kWideRounds; ++rounds) {
-    if (items > kWideGroups * rounds) continue;
-    int lo = kLeastTiles, hi = longest;  // the smallest tps that fits is in lo .. hi
-    while (lo < hi) {
-      const int mid = (lo + hi) >> 1;
-      if (count(mid) <= kWideGroups * rounds) hi = mid;
-      else lo = mid + 1;
-    }
-    const long long s = (long long)rounds * (lo + kSplitCost);
-    if (lo < longest && s < span) {
-      span = s;
-      best = lo;
-    }
+  longest = __builtin_amdgcn_readfirstlane(longest);
+  int lo = kLeastTiles, hi = longest;  // the smallest that fits is in lo .. hi
+  while (lo < hi) {
+    const int mid = (lo + hi) >> 1;
+    if (count(mid) <= kWideUnits) hi = mid;
+    else lo = mid + 1;
   }
-  return __builtin_amdgcn_readfirstlane(best);
+  return lo + kSplitCost < longest ? lo : kWhole;
 }
 
-// Workgroup i takes the pieces i, i + gridDim, ...: piece x * heads + g is item x
-// of cached head g.  A block's last rows, if at most 128, take the form with two
-// key groups.
+// Workgroup x * heads + g: item x of cached head g, the longest sequences' first.  A
+// block's last rows, if at most 128, take the form with two key groups.
 template <int DK, int DV, int KV>
 __global__ __launch_bounds__(512) void paged_wide_kernel(PagedArgs a, ReadArgs r) {
   using C1 = Cfg<DK, DV, 8, kFem, true, false, 1>;
@@ -542,20 +531,18 @@ __global__ __launch_bounds__(512) void paged_wide_kernel(PagedArgs a, ReadArgs r
   const Work w = wide_work(a, r);
   const int tps = wide_tiles(a, r, w);
   if (r.split_wide && blockIdx.x == 0 && threadIdx.x == 0) r.tps[1] = tps;
-  for (int piece = blockIdx.x;; piece += gridDim.x) {
-    const int g = piece % a.heads;
-    const RowItem it = find_item<true>(a, w, tps, piece / a.heads);
-    if (!it.found) return;
-    __syncthreads();  // the last piece's LDS is free
-    if (!it.seq.ok || it.seq.len == 0) {
-      all_nan<DV>(r, it, g, kWideRows, 512);
-      continue;
-    }
-    const long long nr = (long long)it.seq.n * r.G - (long long)it.rb * kWideRows;
-    const int nneed = lo_channels<C1>(r.beta + g * DV, threadIdx.x & 63);
-    if (nr > kWideRows / 2) wide_nlo<C1, KV, 0>((nneed + 31) >> 5, a, r, it, g, piece, smem, nneed);
-    else wide_nlo<C2, KV, 0>((nneed + 31) >> 5, a, r, it, g, piece, smem, nneed);
+  const int g = blockIdx.x % a.heads;
+  const RowItem it = find_item<true>(a, w, tps, blockIdx.x / a.heads);
+  if (!it.found) return;
+  if (!it.seq.ok || it.seq.len == 0) {
+    all_nan<DV>(r, it, g, kWideRows, 512);
+    return;
   }
+  const long long nr = (long long)it.seq.n * r.G - (long long)it.rb * kWideRows;
+  const int nneed = lo_channels<C1>(r.beta + g * DV, threadIdx.x & 63);
+  const int slot = (int)blockIdx.x;
+  if (nr > kWideRows / 2) wide_nlo<C1, KV, 0>((nneed + 31) >> 5, a, r, it, g, slot, smem, nneed);
+  else wide_nlo<C2, KV, 0>((nneed + 31) >> 5, a, r, it, g, slot, smem, nneed);
 }
 
 }  // namespace
