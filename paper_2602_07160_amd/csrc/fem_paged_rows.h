@@ -44,7 +44,7 @@ namespace fem {
 // kernel for at most 16 rb rows leave room for.
 constexpr int row_waves(int dk, int dv, int kv, int rb) {
   if (rb == 2) return dk == 32 ? 3 : 2;
-  return dk == 32 ? 4 : dk == 64 || kv != FEM_KV_BF16 ? 3 : 2;
+  return dk == 32 ? 4 : dv == 128 && kv == FEM_KV_BF16 ? 2 : 3;
 }
 
 constexpr int kRowsMax = 32;       // query rows of a block
@@ -251,15 +251,6 @@ struct RowCfg {
   static constexpr int AREA = VT > MT ? VT : MT;
 };
 
-// Stored bytes of a tile in registers.
-template <int W, int KV>
-struct Stored {
-  // K: per 16-key block and k-step (32 channels), 8 values of the lane's key
-  // V: per 16-key block, 16-byte pieces in memory order
-  static constexpr int KN = W / 32;
-  static constexpr int VN = KV == FEM_KV_BF16 ? W / 32 : (W + 63) / 64;
-};
-
 template <int DK, int DV, int KV, int RB>
 struct RowRead {
   using C = RowCfg<DK, DV>;
@@ -282,70 +273,84 @@ struct RowRead {
   unsigned lo_blocks;  // bit cb: a channel of the block takes hi + lo
 
   u32x4 kw[2][KN];        // bf16: 8 values; 8-bit: words 0, 1 hold 8 codes
-  unsigned ksc[2][KN];
+  unsigned ksc[2];        // scale bytes of the lane's key
   u32x4 vw[2][VN];
   unsigned vsc[2][VN];
 
   __device__ __forceinline__ RowRead(const PagedArgs& a_) : a(a_) {}
 
-  // First row of the 16-key block at key k (inside one page), clamped to the
-  // last block that has visible keys.
-  __device__ __forceinline__ size_t block_row(int k) {
-    const int kk = min(k, (n_eff - 1) & ~15);
-    int p = a.table[(size_t)b * a.table_len + (kk >> a.page_log2)];
-    p = __builtin_amdgcn_readfirstlane(p);
+  // Pages of this wave's next 32 tiles (lane 2 n + kb: 16-key block kb of its n-th
+  // tile from tile t on), so that the loop waits for no page number.  Blocks past the
+  // last visible key stand for the last one.
+  int pages;
+  __device__ __forceinline__ int block_key(int t, int kb) const {
+    return min(t * kRowTile + kb * 16, (n_eff - 1) & ~15);
+  }
+  __device__ __forceinline__ void load_pages(int t) {
+    const int k = block_key(min(t + (lane >> 1) * kRowWaves, 1 << 25), lane & 1);
+    pages = a.table[(size_t)b * a.table_len + (k >> a.page_log2)];
+  }
+  // First row of block kb of tile t, the n-th of those.
+  __device__ __forceinline__ size_t block_row(int t, int kb, int n) {
+    int p = __builtin_amdgcn_readlane(pages, 2 * n + kb);
     if ((unsigned)p >= (unsigned)a.pages) {
       bad = true;
       p = 0;
     }
-    return (((size_t)p * a.heads + g) << a.page_log2) + (kk & (a.page - 1));
+    return (((size_t)p * a.heads + g) << a.page_log2) + (block_key(t, kb) & (a.page - 1));
+  }
+  __device__ __forceinline__ void load(int t, int n) {
+    const size_t row[2] = {block_row(t, 0, n), block_row(t, 1, n)};
+    load_k(row);
+    load_v(row);
   }
 
+  // Lane offsets in a block: the loads take them with a scalar base each.
+  unsigned koff, ksoff, voff, vsoff;
+  __device__ __forceinline__ void lane_offsets() {
+    koff = MX ? l16 * DK + grp * 8 : l16 * (DK * 2) + grp * 16;
+    ksoff = l16 * KN;
+    const unsigned piece = MX && DV == 32 ? lane & 31 : lane;  // 16 bytes of V's rows in order
+    voff = piece * 16;
+    vsoff = piece >> 1;
+  }
   __device__ __forceinline__ void load_k(const size_t (&row)[2]) {
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb) {
-      if constexpr (!MX) {
-        const uint8_t* p = a.k + row[kb] * (DK * 2);
+      const uint8_t* p = a.k + row[kb] * (MX ? DK : DK * 2);
 #pragma unroll
-        for (int ks = 0; ks < KN; ++ks)
-          kw[kb][ks] = *reinterpret_cast<const u32x4*>(p + l16 * (DK * 2) + ks * 64 + grp * 16);
-      } else {
-        const uint8_t* p = a.k + row[kb] * DK;
-        const uint8_t* sp = a.ks + row[kb] * (DK / kScaleBlock);
-#pragma unroll
-        for (int ks = 0; ks < KN; ++ks) {
-          const u32x2v w = *reinterpret_cast<const u32x2v*>(p + l16 * DK + ks * 32 + grp * 8);
+      for (int ks = 0; ks < KN; ++ks) {
+        if constexpr (!MX) {
+          kw[kb][ks] = *reinterpret_cast<const u32x4*>(p + koff + ks * 64);
+        } else {
+          const u32x2v w = *reinterpret_cast<const u32x2v*>(p + koff + ks * 32);
           kw[kb][ks][0] = w[0];
           kw[kb][ks][1] = w[1];
-          ksc[kb][ks] = sp[l16 * (DK / kScaleBlock) + ks];
         }
+      }
+      if constexpr (MX) {
+        const uint8_t* sp = a.ks + row[kb] * KN + ksoff;
+        if constexpr (KN == 4) ksc[kb] = *reinterpret_cast<const unsigned*>(sp);
+        else if constexpr (KN == 2) ksc[kb] = *reinterpret_cast<const unsigned short*>(sp);
+        else ksc[kb] = *sp;
       }
     }
   }
   __device__ __forceinline__ void load_v(const size_t (&row)[2]) {
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb) {
-      if constexpr (!MX) {
-        const uint8_t* p = a.v + row[kb] * (DV * 2);
+      const uint8_t* p = a.v + row[kb] * (MX ? DV : DV * 2);
 #pragma unroll
-        for (int i = 0; i < VN; ++i)
-          vw[kb][i] = *reinterpret_cast<const u32x4*>(p + (i * 64 + lane) * 16);
-      } else {
-        const uint8_t* p = a.v + row[kb] * DV;
-        const uint8_t* sp = a.vs + row[kb] * (DV / kScaleBlock);
-#pragma unroll
-        for (int i = 0; i < VN; ++i) {
-          const int piece = DV == 32 ? lane & 31 : i * 64 + lane;  // of 16 codes
-          vw[kb][i] = *reinterpret_cast<const u32x4*>(p + piece * 16);
-          vsc[kb][i] = sp[piece >> 1];
-        }
+      for (int i = 0; i < VN; ++i) {
+        vw[kb][i] = *reinterpret_cast<const u32x4*>(p + voff + i * 1024);
+        if constexpr (MX) vsc[kb][i] = a.vs[row[kb] * (DV / kScaleBlock) + i * 32 + vsoff];
       }
     }
   }
   __device__ __forceinline__ bf16x8 k_frag(int kb, int ks) const {
     if constexpr (!MX) return __builtin_bit_cast(bf16x8, kw[kb][ks]);
     return __builtin_bit_cast(bf16x8, dequant8<KV>(kw[kb][ks][0], kw[kb][ks][1],
-                                                   scale_of(ksc[kb][ks])));
+                                                   scale_of(ksc[kb] >> (8 * ks) & 0xffu)));
   }
   // The tile's V into LDS as [32][DV] bf16; rows at or past `live` become -inf
   // (E = 0 there, and the column maximum does not see them).
@@ -363,7 +368,7 @@ struct RowRead {
           *reinterpret_cast<u32x4*>(vt + row * C::VROW + col * 16) = w;
         } else {
           constexpr int PPR = DV / 16;
-          const int piece = DV == 32 ? lane & 31 : i * 64 + lane;
+          const int piece = DV == 32 ? lane & 31 : i * 64 + lane;  // as loaded
           const int row = kb * 16 + piece / PPR, col = piece % PPR;
           const float s = scale_of(vsc[kb][i]);
           u32x4 w0 = dequant8<KV>(vw[kb][i][0], vw[kb][i][1], s);
@@ -384,7 +389,7 @@ struct RowRead {
   // lim[rb]: keys that the lane's row sees.  The next tile's rows are loaded
   // where `more` is set.
   __device__ __forceinline__ void tile(int k0, bool masked, const int (&lim)[RB], bool more,
-                                       int knext, float scale2) {
+                                       int tnext, int nnext, float scale2) {
     // ---- S^T = K Q^T
     f32x4 s[RB][2];
 #pragma unroll
@@ -400,11 +405,7 @@ struct RowRead {
       }
     }
     store_v(n_eff - k0);
-    if (more) {
-      const size_t row[2] = {block_row(knext), block_row(knext + 16)};
-      load_k(row);
-      load_v(row);
-    }
+    if (more) load(tnext, nnext);
 
     // ---- P, in the A operand's layout: row l16, keys 4 grp + i, 16 + 4 grp + i
     bf16x8 p[RB];
@@ -558,6 +559,7 @@ __device__ __forceinline__ void rows_body(const PagedArgs& a, const ReadArgs& r,
   w.l16 = tid & 15;
   w.grp = (tid & 63) >> 4;
   w.vt = smem + wave * C::AREA;
+  w.lane_offsets();
   w.b = it.b;
   w.g = g;
   const Seq& sq = it.seq;
@@ -571,9 +573,8 @@ __device__ __forceinline__ void rows_body(const PagedArgs& a, const ReadArgs& r,
 
   int t = tb + wave;
   if (t < te) {
-    const size_t row[2] = {w.block_row(t * kRowTile), w.block_row(t * kRowTile + 16)};
-    w.load_k(row);
-    w.load_v(row);
+    w.load_pages(t);
+    w.load(t, 0);
   }
   int lim[RB];
 #pragma unroll
@@ -598,9 +599,10 @@ __device__ __forceinline__ void rows_body(const PagedArgs& a, const ReadArgs& r,
     w.c[cb] = kNone;
     if (__any(!(b >= kLoBelow))) w.lo_blocks |= 1u << cb;
   }
-  for (; t < te; t += kRowWaves) {
-    const int k0 = t * kRowTile;
-    w.tile(k0, k0 + kRowTile > least, lim, t + kRowWaves < te, (t + kRowWaves) * kRowTile, scale2);
+  for (int n = 1; t < te; t += kRowWaves, n = (n + 1) & 31) {
+    const int k0 = t * kRowTile, next = t + kRowWaves;
+    if (n == 0 && next < te) w.load_pages(next);
+    w.tile(k0, k0 + kRowTile > least, lim, next < te, next, n, scale2);
   }
 
   // ---- the four waves meet: common frames M (row) and Cc (channel)
