@@ -472,7 +472,7 @@ class PagedCache:
         if any(x is not None and x.device != k.device for x in (v, k_scale, v_scale)):
             raise ValueError("the pools must be on one device")
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
-        self.device = k.device
+        self.device, self.index = k.device, k.get_device()
         pages, self.heads, page, self.d_qk = k.shape
         self.d_v = v.shape[3]
         self.c = _Cache(k.data_ptr(), v.data_ptr(), None if k_scale is None else k_scale.data_ptr(),
@@ -510,7 +510,8 @@ class PagedBatch:
         if any(x is not None and x.device != lens.device for x in (q_start, table)):
             raise ValueError("q_start, lens and table must be on one device")
         self.q_start, self.lens, self.table = q_start, lens, table
-        self.device = lens.device
+        self.device, self.index = lens.device, lens.get_device()
+        self.n_seq = lens.shape[0]
         self.n_tok = 0 if n_tok is None else int(n_tok)
         self.c = _Batch(None if q_start is None else q_start.data_ptr(), lens.data_ptr(),
                         table.data_ptr(), lens.shape[0], table.shape[1], self.n_tok,
@@ -519,26 +520,27 @@ class PagedBatch:
 
 
 def _paged(cache, batch):
-    if not isinstance(cache, PagedCache) or not isinstance(batch, PagedBatch):
+    if type(cache) is not PagedCache or type(batch) is not PagedBatch:
         raise ValueError("cache must be a PagedCache and batch a PagedBatch")
-    if cache.device != batch.device:
+    if cache.index != batch.index:
         raise ValueError("cache and batch must be on one device")
 
 
-def _packed(x, name, n_tok, heads, width, device):
+def _packed(x, name, n_tok, heads, width, index):
     """Row stride of a packed [n_tok, heads, width] bf16 tensor whose tokens may
     lie apart (a slice of one projection's output)."""
-    if not isinstance(x, torch.Tensor) or not x.is_cuda or x.device != device:
+    if not isinstance(x, torch.Tensor) or x.get_device() != index:
         raise ValueError(f"{name} must be a GPU tensor on the cache's device")
     if x.dtype != torch.bfloat16:
         raise ValueError(f"{name} must be bfloat16, got {x.dtype}")
-    if x.dim() != 3 or x.shape[0] != n_tok or x.shape[2] != width or \
-            (heads is not None and x.shape[1] != heads):
+    shape = x.shape
+    if len(shape) != 3 or shape[0] != n_tok or shape[2] != width or \
+            (heads is not None and shape[1] != heads):
         raise ValueError(f"{name} must be [n_tok, heads, width] of the batch and the cache")
     s0, s1, s2 = x.stride()
-    if (s2 != 1 and width > 1) or (s1 != width and x.shape[1] > 1):
+    if s2 != 1 or (s1 != width and shape[1] > 1):
         raise ValueError(f"a token's heads must be contiguous in {name}")
-    return s0 if n_tok > 1 else x.shape[1] * width
+    return s0 if n_tok > 1 else shape[1] * width
 
 
 def fem_cache_append(cache, batch, k, v, stream=None) -> None:
@@ -547,12 +549,26 @@ def fem_cache_append(cache, batch, k, v, stream=None) -> None:
     are."""
     lib = load()
     _paged(cache, batch)
-    kld = _packed(k, "k", batch.n_tok, cache.heads, cache.d_qk, cache.device)
-    vld = _packed(v, "v", batch.n_tok, cache.heads, cache.d_v, cache.device)
+    kld = _packed(k, "k", batch.n_tok, cache.heads, cache.d_qk, cache.index)
+    vld = _packed(v, "v", batch.n_tok, cache.heads, cache.d_v, cache.index)
     with _on(cache.device):
         rc = lib.fem_cache_append(cache.ref, batch.ref, k.data_ptr(), kld, v.data_ptr(), vld,
                                   _stream_handle(cache.device, stream))
     _check(rc)
+
+
+def _gathered(x, name, B, H, L, w, cache, stream):
+    """The caller's buffer of a read-back, or a new one of zeros made on its stream."""
+    if x is None:
+        s = torch.cuda.current_stream(cache.device) if stream is None else stream
+        if not isinstance(s, torch.cuda.Stream):
+            s = torch.cuda.ExternalStream(int(s), device=cache.device)
+        with torch.cuda.stream(s):
+            return torch.zeros((B, H, L, w), device=cache.device, dtype=torch.bfloat16)
+    _dev_tensor(x, name, torch.bfloat16)
+    if x.shape != (B, H, L, w) or x.get_device() != cache.index:
+        raise ValueError(f"{name} must be [B, heads, L, width] on the cache's device")
+    return x
 
 
 def fem_cache_gather(cache, batch, k=None, v=None, L=None, stream=None):
@@ -562,27 +578,22 @@ def fem_cache_gather(cache, batch, k=None, v=None, L=None, stream=None):
     the table's length in tokens).  Returns (k, v)."""
     lib = load()
     _paged(cache, batch)
-    B, H = batch.c.n_seq, cache.heads
+    B, H = batch.n_seq, cache.heads
     if L is None:
         given = k if k is not None else v
-        L = batch.c.table_len * cache.c.page if given is None else given.shape[2]
-    s = torch.cuda.current_stream(cache.device) if stream is None else stream
-    out = []
-    for name, x, w in (("k", k, cache.d_qk), ("v", v, cache.d_v)):
-        if x is None:
-            if not isinstance(s, torch.cuda.Stream):
-                s = torch.cuda.ExternalStream(int(s), device=cache.device)
-            with torch.cuda.stream(s):
-                x = torch.zeros((B, H, L, w), device=cache.device, dtype=torch.bfloat16)
-        _dev_tensor(x, name, torch.bfloat16)
-        if tuple(x.shape) != (B, H, L, w) or x.device != cache.device:
-            raise ValueError(f"{name} must be [B, heads, L, width] on the cache's device")
-        out.append(x)
+        if given is None:
+            L = batch.c.table_len * cache.c.page
+        elif not isinstance(given, torch.Tensor) or given.dim() != 4:
+            raise ValueError("k and v must be [B, heads, L, width]")
+        else:
+            L = given.shape[2]
+    k = _gathered(k, "k", B, H, L, cache.d_qk, cache, stream)
+    v = _gathered(v, "v", B, H, L, cache.d_v, cache, stream)
     with _on(cache.device):
-        rc = lib.fem_cache_gather(cache.ref, batch.ref, out[0].data_ptr(), out[1].data_ptr(), L,
+        rc = lib.fem_cache_gather(cache.ref, batch.ref, k.data_ptr(), v.data_ptr(), L,
                                   _stream_handle(cache.device, stream))
     _check(rc)
-    return out[0], out[1]
+    return k, v
 
 
 def fem_paged_workspace_bytes(cache, batch, H) -> int:
@@ -601,10 +612,10 @@ def fem_paged_fwd(cache, batch, q, beta, causal: bool = True, out=None, out_dtyp
     (out's type, or out_dtype)."""
     lib = load()
     _paged(cache, batch)
-    qld = _packed(q, "q", batch.n_tok, None, cache.d_qk, cache.device)
+    qld = _packed(q, "q", batch.n_tok, None, cache.d_qk, cache.index)
     H = q.shape[1]
     _dev_tensor(beta, "beta", torch.float32)
-    if tuple(beta.shape) != (cache.heads, cache.d_v) or beta.device != cache.device:
+    if beta.shape != (cache.heads, cache.d_v) or beta.get_device() != cache.index:
         raise ValueError("beta must be [heads, d_v] on the cache's device")
     if out is not None:
         out_dtype = out.dtype
@@ -613,7 +624,7 @@ def fem_paged_fwd(cache, batch, q, beta, causal: bool = True, out=None, out_dtyp
     if out is None:
         out = torch.empty((batch.n_tok, H, cache.d_v), device=cache.device, dtype=out_dtype)
     _dev_tensor(out, "out", out_dtype)
-    if tuple(out.shape) != (batch.n_tok, H, cache.d_v) or out.device != cache.device:
+    if out.shape != (batch.n_tok, H, cache.d_v) or out.get_device() != cache.index:
         raise ValueError("out must be [n_tok, H, d_v] on the cache's device")
     flags = (0 if causal else FEM_FLAG_ENCODER) | \
         (FEM_FLAG_OUT_BF16 if out_dtype == torch.bfloat16 else 0)

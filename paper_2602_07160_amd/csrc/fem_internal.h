@@ -103,6 +103,7 @@ struct PagedPlan {
   long long wide_least;    //   rows > wide_least
   int row_blocks, target;  // few rows: bound of the row blocks of a cached head, and of
                            //   the splits over all heads (0: nothing is split)
+  int waves;               //   waves of a workgroup
   int wide_blocks;         // many rows: bound of a cached head's row blocks
   bool split_wide;
   int rps, wide_rps;       // rows of a slot

@@ -9,7 +9,9 @@ namespace fem {
 
 namespace {
 constexpr int kUnits = 256;      // compute units
-constexpr int kShortKeys = 512;  // contexts that are not split: four tiles a wave
+// Contexts that are not split: eight waves have four tiles each at most, which
+// takes about as long as the merge of splits would (B1 H8 L701 d64: KSHORT).
+constexpr int kShortKeys = 1024;
 constexpr int kMergeRows = 4, kWideMergeRows = 16;  // of a merge's workgroup
 
 size_t up256(size_t x) { return (x + 255) / 256 * 256; }
@@ -34,8 +36,10 @@ PagedPlan paged_plan(const PagedArgs& a, int H, int dk, int dv, int kv) {
     const long long m = std::min<long long>(most, kRowsMax);
     p.row_blocks = blocks(m, kRowsMax);
     p.rps = (int)m;
-    const int room = kUnits * row_waves(dk, dv, kv, m <= 16 ? 1 : 2);
-    p.target = keys <= kShortKeys ? 0 : room;
+    const bool brief = keys <= kShortKeys;
+    p.waves = brief ? 2 * kRowWaves : kRowWaves;
+    const int room = kUnits * (brief ? 1 : row_waves(dk, dv, kv, m <= 16 ? 1 : 2));
+    p.target = brief ? 0 : room;
     p.groups = p.target ? room : std::min<size_t>((size_t)p.row_blocks * a.heads, room);
     if (p.target) at += up256((size_t)p.target * p.rps * (dv + 1) * sizeof(float));
   }

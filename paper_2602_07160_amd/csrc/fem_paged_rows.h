@@ -49,8 +49,8 @@ constexpr int row_waves(int dk, int dv, int kv, int rb) {
 
 constexpr int kRowsMax = 32;       // query rows of a block
 constexpr int kRowTile = 32;       // keys of a wave's tile
-constexpr int kRowWaves = 4;
-constexpr int kRowThreads = 64 * kRowWaves;
+constexpr int kRowWaves = 4;       // of a workgroup; calls with short contexts take twice as
+                                   // many and do not split (kShortKeys)
 constexpr float kRowBias = 40.f;   // of P and of E
 constexpr float kLag = 8.f;        // of m and of c
 constexpr float kNone = -1e30f;    // m and c before the first key: finite, so that a hidden
@@ -251,7 +251,8 @@ struct RowCfg {
   static constexpr int AREA = VT > MT ? VT : MT;
 };
 
-template <int DK, int DV, int KV, int RB>
+// One wave's part of a read; NW waves share the keys.
+template <int DK, int DV, int KV, int RB, int NW>
 struct RowRead {
   using C = RowCfg<DK, DV>;
   static constexpr bool MX = KV != FEM_KV_BF16;
@@ -268,7 +269,8 @@ struct RowRead {
 
   bf16x8 qf[RB][C::NKS];
   f32x4 acc[RB][C::NCB];
-  float m[RB], lsum[RB];
+  float m[RB];
+  f32x4 lsum[RB];  // sums of rows 4 grp + i, the same in every lane of the group
   float bl[C::NCB], c[C::NCB];
   unsigned lo_blocks;  // bit cb: a channel of the block takes hi + lo
 
@@ -287,7 +289,7 @@ struct RowRead {
     return min(t * kRowTile + kb * 16, (n_eff - 1) & ~15);
   }
   __device__ __forceinline__ void load_pages(int t) {
-    const int k = block_key(min(t + (lane >> 1) * kRowWaves, 1 << 25), lane & 1);
+    const int k = block_key(min(t + (lane >> 1) * NW, 1 << 25), lane & 1);
     pages = a.table[(size_t)b * a.table_len + (k >> a.page_log2)];
   }
   // First row of block kb of tile t, the n-th of those.
@@ -408,42 +410,49 @@ struct RowRead {
     if (more) load(tnext, nnext);
 
     // ---- P, in the A operand's layout: row l16, keys 4 grp + i, 16 + 4 grp + i
-    bf16x8 p[RB];
+    bf16x8 p[RB], ones;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) ones[e] = (__bf16)1.f;
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
       float x[8];
+      auto exponents = [&] {
+        const float sh = kRowBias - m[rb];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] = s[rb][e >> 2][e & 3] * scale2;
+        for (int e = 0; e < 8; ++e) x[e] = fmaf(s[rb][e >> 2][e & 3], scale2, sh);
+        return max8(x);
+      };
       if (masked) {
         const int left = lim[rb] - k0 - 4 * grp;
 #pragma unroll
         for (int e = 0; e < 8; ++e)
-          if ((e & 3) + 16 * (e >> 2) >= left) x[e] = -INFINITY;
+          if ((e & 3) + 16 * (e >> 2) >= left) s[rb][e >> 2][e & 3] = -INFINITY;
       }
-      float mx = max8(x);
-      if (__any(mx > m[rb] + kLag)) {
+      if (__any(exponents() > kRowBias + kLag)) {
+        float mx = fmaxf(fmaxf(fmaxf(s[rb][0][0], s[rb][0][1]), fmaxf(s[rb][0][2], s[rb][0][3])),
+                         fmaxf(fmaxf(s[rb][1][0], s[rb][1][1]), fmaxf(s[rb][1][2], s[rb][1][3])));
         mx = fmaxf(mx, __shfl_xor(mx, 16));
-        mx = fmaxf(mx, __shfl_xor(mx, 32));
+        mx = fmaxf(mx, __shfl_xor(mx, 32)) * scale2;
         const float mn = mx > m[rb] + kLag ? mx : m[rb];
         const float f = mn == m[rb] ? 1.f : exp2_hw(m[rb] - mn);
         m[rb] = mn;
-        lsum[rb] *= f;
         f32x4 fr;
 #pragma unroll
         for (int i = 0; i < 4; ++i) fr[i] = __shfl(f, 4 * grp + i);
+        lsum[rb] *= fr;
 #pragma unroll
         for (int cb = 0; cb < C::NCB; ++cb) acc[rb][cb] *= fr;
+        exponents();
       }
-      const float sh = kRowBias - m[rb];
 #pragma unroll
       for (int e = 0; e < 8; e += 2) {
-        // rounded to bf16 (2^-9 relative); lsum adds the same rounded values,
-        // so the rounding cancels from the mean over the keys
-        const bf16x2 p2 = to_bf16x2(exp2_hw(x[e] + sh), exp2_hw(x[e + 1] + sh));
+        // rounded to bf16 (at most 2^-8 relative); lsum adds the same rounded
+        // values, so the rounding cancels from the mean over the keys
+        const bf16x2 p2 = to_bf16x2(exp2_hw(x[e]), exp2_hw(x[e + 1]));
         p[rb][e] = p2[0];
         p[rb][e + 1] = p2[1];
-        lsum[rb] = add_bf16x2(p2, lsum[rb]);
       }
+      lsum[rb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(p[rb], ones, lsum[rb], 0, 0, 0);
     }
 
     // ---- E and O += P E, 16 channels at a time
@@ -549,11 +558,11 @@ __device__ __forceinline__ void put(const ReadArgs& r, size_t at, float x) {
 }
 
 // The read of one split of one row block (at most 16 RB rows) of cached head g.
-template <int DK, int DV, int KV, int RB>
+template <int DK, int DV, int KV, int RB, int NW>
 __device__ __forceinline__ void rows_body(const PagedArgs& a, const ReadArgs& r, const RowItem& it,
                                           int g, int slot, unsigned char* smem) {
   using C = RowCfg<DK, DV>;
-  RowRead<DK, DV, KV, RB> w(a);
+  RowRead<DK, DV, KV, RB, NW> w(a);
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   w.lane = tid & 63;
   w.l16 = tid & 15;
@@ -586,7 +595,7 @@ __device__ __forceinline__ void rows_body(const PagedArgs& a, const ReadArgs& r,
     for (int ks = 0; ks < C::NKS; ++ks) w.qf[rb][ks] = *reinterpret_cast<const bf16x8*>(qp + ks * 32);
     lim[rb] = row_limit(sq, row, r.G, causal);
     w.m[rb] = kNone;
-    w.lsum[rb] = 0.f;
+    w.lsum[rb] = f32x4{};
 #pragma unroll
     for (int cb = 0; cb < C::NCB; ++cb) w.acc[rb][cb] = f32x4{};
   }
@@ -599,25 +608,23 @@ __device__ __forceinline__ void rows_body(const PagedArgs& a, const ReadArgs& r,
     w.c[cb] = kNone;
     if (__any(!(b >= kLoBelow))) w.lo_blocks |= 1u << cb;
   }
-  for (int n = 1; t < te; t += kRowWaves, n = (n + 1) & 31) {
-    const int k0 = t * kRowTile, next = t + kRowWaves;
+  for (int n = 1; t < te; t += NW, n = (n + 1) & 31) {
+    const int k0 = t * kRowTile, next = t + NW;
     if (n == 0 && next < te) w.load_pages(next);
     w.tile(k0, k0 + kRowTile > least, lim, next < te, next, n, scale2);
   }
 
-  // ---- the four waves meet: common frames M (row) and Cc (channel)
-  float* const fm = reinterpret_cast<float*>(smem + kRowWaves * C::AREA);  // [4][32] row maxima
-  float* const fl = fm + kRowWaves * kRowsMax;                            // [4][32] row sums
-  float* const fc = fl + kRowWaves * kRowsMax;                            // [4][DV] shifts
-  int* const fbad = reinterpret_cast<int*>(fc + kRowWaves * DV);           // [4]
+  // ---- the waves meet: common frames M (row) and Cc (channel)
+  float* const fm = reinterpret_cast<float*>(smem + NW * C::AREA);  // [NW][32] row maxima
+  float* const fl = fm + NW * kRowsMax;                            // [NW][32] row sums
+  float* const fc = fl + NW * kRowsMax;                            // [NW][DV] shifts
+  int* const fbad = reinterpret_cast<int*>(fc + NW * DV);           // [NW]
 #pragma unroll
   for (int rb = 0; rb < RB; ++rb) {
-    float l = w.lsum[rb];
-    l += __shfl_xor(l, 16);
-    l += __shfl_xor(l, 32);
-    if (w.grp == 0) {
-      fm[wave * kRowsMax + rb * 16 + w.l16] = w.m[rb];
-      fl[wave * kRowsMax + rb * 16 + w.l16] = l;
+    if (w.grp == 0) fm[wave * kRowsMax + rb * 16 + w.l16] = w.m[rb];
+    if (w.l16 == 0) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) fl[wave * kRowsMax + rb * 16 + 4 * w.grp + i] = w.lsum[rb][i];
     }
   }
   if (w.grp == 0) {
@@ -626,14 +633,20 @@ __device__ __forceinline__ void rows_body(const PagedArgs& a, const ReadArgs& r,
   }
   if (w.lane == 0) fbad[wave] = w.bad;
   __syncthreads();
-  const bool bad = (fbad[0] | fbad[1] | fbad[2] | fbad[3]) != 0;
-  auto top4 = [](const float* p, int stride) {
-    return fmaxf(fmaxf(p[0], p[stride]), fmaxf(p[2 * stride], p[3 * stride]));
+  int any_bad = 0;
+#pragma unroll
+  for (int x = 0; x < NW; ++x) any_bad |= fbad[x];
+  const bool bad = any_bad != 0;
+  auto top_of = [](const float* p, int stride) {  // over the waves
+    float t = p[0];
+#pragma unroll
+    for (int x = 1; x < NW; ++x) t = fmaxf(t, p[x * stride]);
+    return t;
   };
   float cf[C::NCB];
 #pragma unroll
   for (int cb = 0; cb < C::NCB; ++cb) {
-    const float top = top4(fc + cb * 16 + w.l16, DV);
+    const float top = top_of(fc + cb * 16 + w.l16, DV);
     cf[cb] = exp2_hw(w.c[cb] - top);
   }
 #pragma unroll
@@ -643,7 +656,7 @@ __device__ __forceinline__ void rows_body(const PagedArgs& a, const ReadArgs& r,
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int q = rb * 16 + 4 * w.grp + i;
-      rf[i] = exp2_hw(fm[wave * kRowsMax + q] - top4(fm + q, kRowsMax));
+      rf[i] = exp2_hw(fm[wave * kRowsMax + q] - top_of(fm + q, kRowsMax));
     }
     float* area = reinterpret_cast<float*>(smem + wave * C::AREA);
 #pragma unroll
@@ -654,14 +667,14 @@ __device__ __forceinline__ void rows_body(const PagedArgs& a, const ReadArgs& r,
     }
     __syncthreads();
     const int kbeg = tb * kRowTile, kend = min(te * kRowTile, w.n_eff);
-    for (int e = tid; e < 16 * DV; e += kRowThreads) {
+    for (int e = tid; e < 16 * DV; e += 64 * NW) {
       const int q = e / DV, j = e % DV, row = r0 + rb * 16 + q;
       if (rb * 16 + (e & ~63) / DV >= nr) break;  // the wave's rows are past the last
       const bool live = rb * 16 + q < nr;
-      const float M = top4(fm + rb * 16 + q, kRowsMax), top = top4(fc + j, DV);
+      const float M = top_of(fm + rb * 16 + q, kRowsMax), top = top_of(fc + j, DV);
       float sum = 0.f, l = 0.f;
 #pragma unroll
-      for (int x = 0; x < kRowWaves; ++x) {
+      for (int x = 0; x < NW; ++x) {
         sum += reinterpret_cast<const float*>(smem + x * C::AREA)[q * C::OROW + j];
         l += fl[x * kRowsMax + rb * 16 + q] * exp2_hw(fm[x * kRowsMax + rb * 16 + q] - M);
       }
@@ -715,11 +728,12 @@ __device__ __forceinline__ void all_nan(const ReadArgs& r, const RowItem& it, in
 
 // Workgroup i takes the pieces i, i + gridDim, ...: piece x * heads + g is item x
 // of cached head g.  RB = 1: no sequence has more than 16 rows.
-template <int DK, int DV, int KV, int RB>
-__global__ __launch_bounds__(kRowThreads, row_waves(DK, DV, KV, RB)) void paged_rows_kernel(PagedArgs a, ReadArgs r) {
+template <int DK, int DV, int KV, int RB, int NW>
+__global__ __launch_bounds__(64 * NW, NW == kRowWaves ? row_waves(DK, DV, KV, RB) : 2)
+void paged_rows_kernel(PagedArgs a, ReadArgs r) {
   using C = RowCfg<DK, DV>;
   __shared__ __align__(16) unsigned char
-      smem[kRowWaves * C::AREA + kRowWaves * (2 * kRowsMax + DV) * 4 + 16];
+      smem[NW * (C::AREA + (2 * kRowsMax + DV) * 4 + 4)];
   const Work wk = rows_work(a, r);
   const int tps = tiles_per_split(a, wk, r.target);
   if (r.target != 0 && blockIdx.x == 0 && threadIdx.x == 0) r.tps[0] = tps;
@@ -728,13 +742,13 @@ __global__ __launch_bounds__(kRowThreads, row_waves(DK, DV, KV, RB)) void paged_
     const RowItem it = find_item<true>(a, wk, tps, piece / a.heads);
     if (!it.found) return;
     if (!it.seq.ok || it.seq.len == 0) {
-      all_nan<DV>(r, it, g, kRowsMax, kRowThreads);
+      all_nan<DV>(r, it, g, kRowsMax, 64 * NW);
       continue;
     }
     __syncthreads();  // the last piece's LDS is free
     const long long left = (long long)it.seq.n * r.G - (long long)it.rb * kRowsMax;
-    if (RB == 1 || left <= 16) rows_body<DK, DV, KV, 1>(a, r, it, g, piece, smem);
-    else rows_body<DK, DV, KV, 2>(a, r, it, g, piece, smem);
+    if (RB == 1 || left <= 16) rows_body<DK, DV, KV, 1, NW>(a, r, it, g, piece, smem);
+    else rows_body<DK, DV, KV, 2, NW>(a, r, it, g, piece, smem);
   }
 }
 
