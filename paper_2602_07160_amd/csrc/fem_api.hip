@@ -297,7 +297,7 @@ extern "C" size_t fem_paged_workspace_bytes(const fem_paged_cache* cache,
                                             const fem_paged_batch* batch, int H) {
   fem::PagedArgs a;
   if (paged_args(cache, batch, true, &a) != FEM_OK || paged_heads_ok(a, H) != FEM_OK) return 0;
-  return fem::paged_plan(a, H, cache->d_qk, cache->d_v, cache->type).ws_bytes;
+  return fem::paged_plan(a, H, cache->d_v).ws_bytes;
 }
 
 extern "C" int fem_paged_fwd(const fem_paged_cache* cache, const fem_paged_batch* batch,
@@ -311,7 +311,7 @@ extern "C" int fem_paged_fwd(const fem_paged_cache* cache, const fem_paged_batch
   if (flags & ~(FEM_FLAG_ENCODER | FEM_FLAG_OUT_BF16)) return FEM_ERR_UNSUPPORTED;
   if (!ld_ok(q_ld, (long long)H * cache->d_qk)) return FEM_ERR_SHAPE;
   if (!aligned16(q) || !aligned16(out)) return FEM_ERR_ALIGN;
-  const fem::PagedPlan plan = fem::paged_plan(a, H, cache->d_qk, cache->d_v, cache->type);
+  const fem::PagedPlan plan = fem::paged_plan(a, H, cache->d_v);
   rc = check_ws(ws, ws_bytes, plan.ws_bytes);
   if (rc != FEM_OK) return rc;
   return from_hip(fem::launch_paged_read(a, plan, cache->type, cache->d_qk, cache->d_v, q, q_ld,

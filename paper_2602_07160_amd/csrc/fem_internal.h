@@ -110,7 +110,7 @@ struct PagedPlan {
   size_t groups, wide_groups;  // workgroups
   size_t part_at, wide_at, ws_bytes;
 };
-PagedPlan paged_plan(const PagedArgs& a, int H, int dk, int dv, int kv);
+PagedPlan paged_plan(const PagedArgs& a, int H, int dv);
 hipError_t launch_paged_read(const PagedArgs& a, const PagedPlan& plan, int kv, int dk, int dv,
                              const void* q, long long qld, const float* beta, void* out, int H,
                              bool causal, bool obf16, void* ws, hipStream_t stream);

@@ -12,14 +12,24 @@ constexpr int kUnits = 256;      // compute units
 // Contexts that are not split: eight waves have four tiles each at most, which
 // takes about as long as the merge of splits would (B1 H8 L701 d64: KSHORT).
 constexpr int kShortKeys = 1024;
-constexpr int kMergeRows = 4, kWideMergeRows = 16;  // of a merge's workgroup
+constexpr int kMergeRows = 8;    // of a merge's workgroup, few rows a block
+
+// Rows of a merge's workgroup, many rows a block: as many as leave about four
+// workgroups a compute unit, whose cost is mostly finding their rows (one block of
+// 256 rows and eight heads in 32 splits: 51 us with 8 rows, 59 with 16; ten blocks
+// and twelve heads in two: 64 and 58).
+int wide_merge_rows(size_t rows) {
+  int n = 4;
+  while (n < 16 && rows / (2 * n) >= 4 * kUnits) n *= 2;
+  return n;
+}
 
 size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 }  // namespace
 
 // Up to 32 rows a sequence the kernel for few rows; more, the one for many; both
 // where max_q allows either.
-PagedPlan paged_plan(const PagedArgs& a, int H, int dk, int dv, int kv) {
+PagedPlan paged_plan(const PagedArgs& a, int H, int dv) {
   PagedPlan p = {};
   const long long G = H / a.heads, rows = (long long)a.ntok * G, most = a.max_q * G;
   const long long keys = (long long)a.table_len << a.page_log2;
@@ -38,10 +48,10 @@ PagedPlan paged_plan(const PagedArgs& a, int H, int dk, int dv, int kv) {
     p.rps = (int)m;
     const bool brief = keys <= kShortKeys;
     p.waves = brief ? 2 * kRowWaves : kRowWaves;
-    const int room = kUnits * (brief ? 1 : row_waves(dk, dv, kv, m <= 16 ? 1 : 2));
+    const int room = kUnits * (brief ? 1 : kRowGroups);
     p.target = brief ? 0 : room;
     p.groups = p.target ? room : std::min<size_t>((size_t)p.row_blocks * a.heads, room);
-    if (p.target) at += up256((size_t)p.target * p.rps * (dv + 1) * sizeof(float));
+    if (p.target) at += up256((size_t)p.target * p.rps * part_row(dv) * sizeof(float));
   }
   p.wide_at = at;
   if (p.wide) {
@@ -51,7 +61,7 @@ PagedPlan paged_plan(const PagedArgs& a, int H, int dk, int dv, int kv) {
     p.wide_groups = (size_t)p.wide_blocks * a.heads;
     if (p.split_wide) {
       p.wide_groups = std::max<size_t>(p.wide_groups, kWideUnits);
-      at += up256((size_t)kWideUnits * p.wide_rps * (dv + 1) * sizeof(float));
+      at += up256((size_t)kWideUnits * p.wide_rps * part_row(dv) * sizeof(float));
     }
   }
   p.ws_bytes = p.target || p.split_wide ? at : 0;
@@ -79,8 +89,7 @@ hipError_t launch_paged_read(const PagedArgs& a, const PagedPlan& plan, int kv, 
   r.wide_least = plan.wide_least;
   r.causal = causal;
   r.obf16 = obf16;
-  // A merge's workgroups.  Splits number at most `target` (few rows) or one a
-  // compute unit, and a block that is split has two at least.
+  // The merge's workgroups: calls of more blocks than splits are aimed at are not split.
   MergePart few = {}, many = {};
   if (plan.rows && plan.target) {
     few = MergePart{rows_work(a, r), r.tps, r.part, plan.rps, kMergeRows, 0};
@@ -88,9 +97,10 @@ hipError_t launch_paged_read(const PagedArgs& a, const PagedPlan& plan, int kv, 
     few.groups = (int)(blocks * ((plan.rps + kMergeRows - 1) / kMergeRows));
   }
   if (plan.wide && plan.split_wide) {
-    many = MergePart{wide_work(a, r), r.tps + 1, r.wide_part, plan.wide_rps, kWideMergeRows, 0};
-    const size_t blocks = std::min<size_t>((size_t)plan.wide_blocks * a.heads, kWideUnits);
-    many.groups = (int)(blocks * ((plan.wide_rps + kWideMergeRows - 1) / kWideMergeRows));
+    const size_t blocks = std::min<size_t>((size_t)plan.wide_blocks * a.heads, kMostSplitBlocks);
+    const int n = wide_merge_rows(blocks * plan.wide_rps);
+    many = MergePart{wide_work(a, r), r.tps + 1, r.wide_part, plan.wide_rps, n, 0};
+    many.groups = (int)(blocks * ((plan.wide_rps + n - 1) / n));
   }
   auto go = [&](auto rows, auto wide, auto merge) {
     hipError_t e = hipSuccess;

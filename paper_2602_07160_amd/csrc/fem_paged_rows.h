@@ -40,12 +40,11 @@
 
 namespace fem {
 
-// Waves of a SIMD, that is workgroups of a compute unit, that the registers of the
-// kernel for at most 16 rb rows leave room for.
-constexpr int row_waves(int dk, int dv, int kv, int rb) {
-  if (rb == 2) return dk == 32 ? 3 : 2;
-  return dk == 32 ? 4 : dv == 128 && kv == FEM_KV_BF16 ? 2 : 3;
-}
+// Workgroups of a compute unit (of kRowWaves waves, one a SIMD).  A third one helps
+// nothing: 16 sequences of up to 8192 keys, one token, 8 heads, d = 64, 38.2 us with
+// two and 38.8 with three; e4m3 34.5 and 35.2; d = 128 e4m3, whose registers then
+// spill, 166 and 196 us at 16 x 32768 keys.
+constexpr int kRowGroups = 2;
 
 constexpr int kRowsMax = 32;       // query rows of a block
 constexpr int kRowTile = 32;       // keys of a wave's tile
@@ -70,8 +69,7 @@ struct Work {
   bool longest_first;  // items in the order of falling lengths (up to 64 sequences)
 };
 
-// The split of the work, formed by every wave from the lengths: `tps` key tiles
-// make a split of a row block.
+// A workgroup's piece of the work.
 struct RowItem {
   int b, rb, s, ns;  // sequence, row block, split and the number of splits
   int slot;          // number of split s among those of one head
@@ -80,122 +78,177 @@ struct RowItem {
 };
 
 struct RowCounts {
-  int nrb, nt;
+  int nrb, nt;  // row blocks, and key tiles of one
 };
-
-__device__ __forceinline__ RowCounts row_counts(const Seq& q, const Work& w) {
-  // a sequence that cannot be read is one item, whatever its rows (see all_nan)
-  const bool ok = q.ok && q.n <= w.max_q;
-  const long long rows = ok ? (long long)q.n * w.G : q.n > 0 ? 1 : 0;
-  RowCounts c = {0, 0};
-  if (rows > w.lo && rows <= w.hi) {
-    c.nrb = (int)((rows + w.br - 1) / w.br);
-    c.nt = ok ? max((q.len + w.tk - 1) / w.tk, 1) : 1;
-  }
-  return c;
-}
-
-// Sum over the call's sequences of f(counts), the same in every lane.
-template <class F>
-__device__ __forceinline__ long long sum_items(const PagedArgs& a, const Work& w, F&& f) {
-  const int lane = threadIdx.x & 63;
-  long long t = 0;
-  for (int b0 = 0; b0 < a.nseq; b0 += 64) {
-    const int b = b0 + lane;
-    if (b < a.nseq) t += f(row_counts(seq_of(a, b, w.causal), w));
-  }
-  const int m = min(64, a.nseq);  // lanes with a sequence
-  for (int o = 1; o < m; o <<= 1) t += __shfl_xor(t, o);
-  return (long long)(unsigned)__builtin_amdgcn_readfirstlane((int)t) |
-         (long long)__builtin_amdgcn_readfirstlane((int)(t >> 32)) << 32;
-}
 
 constexpr int kWhole = 1 << 30;  // tiles of a split where nothing is split
 
-// Tiles of a split such that all splits of all heads number at most `target`, the
-// smallest of 64 candidates (a lane each) between a target-th of the tiles and three
-// times that; kWhole where none will do or nothing is to be split.
-__device__ __forceinline__ int tiles_per_split(const PagedArgs& a, const Work& w, int target) {
-  if (target == 0) return kWhole;
-  const int lane = threadIdx.x & 63;
-  const long long t =
-      sum_items(a, w, [](const RowCounts& c) { return (long long)c.nrb * c.nt; }) * a.heads;
-  const long long least = max((t + target - 1) / target, (long long)kRowWaves);
-  const int cand = (int)min(least + (least * lane + 31) / 32, (long long)kWhole);
-  const float inv = 1.f / (float)cand;
-  long long n = 0;  // splits of a head with this lane's candidate
-  for (int b0 = 0; b0 < a.nseq; b0 += 64) {
-    RowCounts c = {0, 0};
-    if (b0 + lane < a.nseq) c = row_counts(seq_of(a, b0 + lane, w.causal), w);
-    const int m = min(64, a.nseq - b0);
-    for (int i = 0; i < m; ++i) {
-      const int nrb = __builtin_amdgcn_readlane(c.nrb, i), nt = __builtin_amdgcn_readlane(c.nt, i);
-      // ceil(nt / cand), or one more where the product rounds up to a whole number
-      n += (long long)nrb * ((int)((float)nt * inv) + 1);
-    }
-  }
-  const uint64_t fits = __ballot(n * a.heads <= target);
-  return fits == 0 ? kWhole : __builtin_amdgcn_readlane(cand, __builtin_ctzll(fits));
-}
+// The split of the work, formed from the lengths by one wave of every workgroup: a
+// lane has a sequence (the first 64 in registers).
+struct Planner {
+  const PagedArgs& a;
+  const Work& w;
+  int lane;
+  RowCounts first;
 
-// Item `x` of all heads' alike: a split of a row block (SPLITS), or a whole row
-// block.  Items are numbered by sequence, row block and split; longest_first takes
-// the sequences by length and a sequence's last row block first.
-template <bool SPLITS>
-__device__ __forceinline__ RowItem find_item(const PagedArgs& a, const Work& w, int tps, int x) {
-  const int lane = threadIdx.x & 63;
-  RowItem it;
-  it.found = false;
-  int base = 0, slot = 0;
-  for (int b0 = 0; b0 < a.nseq; b0 += 64) {
-    const int b = b0 + lane;
+  __device__ __forceinline__ Planner(const PagedArgs& a_, const Work& w_)
+      : a(a_), w(w_), lane(threadIdx.x & 63) {
+    first = fetch(0);
+  }
+  __device__ __forceinline__ RowCounts fetch(int b0) const {
     RowCounts c = {0, 0};
-    if (b < a.nseq) c = row_counts(seq_of(a, b, w.causal), w);
-    const int m64 = min(64, a.nseq - b0);
-    int who = b;  // this lane's sequence
-    if (w.longest_first && a.nseq <= 64) {
-      int rank = lane;
-      if (lane < m64) {
-        rank = 0;
-        for (int i = 0; i < m64; ++i) {
-          const int t = __builtin_amdgcn_readlane(c.nt, i);
-          rank += t > c.nt || (t == c.nt && i < lane);
+    if (b0 + lane >= a.nseq) return c;
+    const Seq q = seq_of(a, b0 + lane, w.causal);
+    // a sequence that cannot be read is one item, whatever its rows (see all_nan)
+    const bool ok = q.ok && q.n <= w.max_q;
+    const long long rows = ok ? (long long)q.n * w.G : q.n > 0 ? 1 : 0;
+    if (rows > w.lo && rows <= w.hi) {
+      c.nrb = (int)((rows + w.br - 1) / w.br);
+      c.nt = ok ? max((q.len + w.tk - 1) / w.tk, 1) : 1;
+    }
+    return c;
+  }
+  __device__ __forceinline__ RowCounts counts(int b0) const { return b0 == 0 ? first : fetch(b0); }
+  __device__ __forceinline__ int lanes(int b0) const { return min(64, a.nseq - b0); }
+
+  // Sum of f(counts) over the sequences and heads, the same in every lane.
+  template <class F>
+  __device__ __forceinline__ long long total(F&& f) const {
+    long long t = 0;
+    for (int b0 = 0; b0 < a.nseq; b0 += 64) t += f(counts(b0));
+    const int m = lanes(0);
+    for (int o = 1; o < m; o <<= 1) t += __shfl_xor(t, o);
+    return ((long long)(unsigned)__builtin_amdgcn_readfirstlane((int)t) |
+            (long long)__builtin_amdgcn_readfirstlane((int)(t >> 32)) << 32) * a.heads;
+  }
+  __device__ __forceinline__ int longest() const {
+    int t = 0;
+    for (int b0 = 0; b0 < a.nseq; b0 += 64) t = max(t, counts(b0).nt);
+    const int m = lanes(0);
+    for (int o = 1; o < m; o <<= 1) t = max(t, __shfl_xor(t, o));
+    return __builtin_amdgcn_readfirstlane(t);
+  }
+
+  // Tiles of a split such that all splits of all heads number at most `target`: the
+  // smallest of 64 candidates (a lane each) between a target-th of the tiles and
+  // three times that; kWhole where none will do or nothing is to be split.
+  __device__ __forceinline__ int tiles_per_split(int target, int least_tiles) const {
+    if (target == 0) return kWhole;
+    const long long t = total([](const RowCounts& c) { return (long long)c.nrb * c.nt; });
+    const long long least = max((t + target - 1) / target, (long long)least_tiles);
+    const int cand = (int)min(least + (least * lane + 31) / 32, (long long)kWhole);
+    const float inv = 1.f / (float)cand;
+    float n = 0.f;  // splits of a head with this lane's candidate (exact up to 2^24)
+    for (int b0 = 0; b0 < a.nseq; b0 += 64) {
+      const RowCounts c = counts(b0);
+      const float nrb = (float)c.nrb, nt = (float)c.nt;
+      const int m = lanes(b0);
+      for (int i = 0; i < m; ++i) {
+        // ceil(nt / cand), or one more where the product rounds up to a whole number
+        n = fmaf(lane_of(nrb, i), floorf(lane_of(nt, i) * inv) + 1.f, n);
+      }
+    }
+    const uint64_t fits = __ballot(n * (float)a.heads <= (float)target);
+    return fits == 0 ? kWhole : __builtin_amdgcn_readlane(cand, __builtin_ctzll(fits));
+  }
+  __device__ __forceinline__ static float lane_of(float x, int i) {
+    return __uint_as_float((unsigned)__builtin_amdgcn_readlane((int)__float_as_uint(x), i));
+  }
+
+  // Item x of all heads' alike: a split of a row block (SPLITS), or a whole row
+  // block.  Items are numbered by sequence, row block and split; longest_first takes
+  // the sequences by length and a sequence's last row block first.
+  template <bool SPLITS>
+  __device__ __forceinline__ RowItem find(int tps, int x) const {
+    RowItem it;
+    it.found = false;
+    int base = 0, slot = 0;
+    for (int b0 = 0; b0 < a.nseq; b0 += 64) {
+      RowCounts c = counts(b0);
+      const int m64 = lanes(b0);
+      int who = b0 + lane;  // this lane's sequence
+      if (w.longest_first && a.nseq <= 64) {
+        int rank = lane;
+        if (lane < m64) {
+          rank = 0;
+          for (int i = 0; i < m64; ++i) {
+            const int t = __builtin_amdgcn_readlane(c.nt, i);
+            rank += t > c.nt || (t == c.nt && i < lane);
+          }
+        }
+        who = __builtin_amdgcn_ds_permute(rank * 4, who);
+        c.nt = __builtin_amdgcn_ds_permute(rank * 4, c.nt);
+        c.nrb = __builtin_amdgcn_ds_permute(rank * 4, c.nrb);
+      }
+      const int nrb = c.nrb, ns = tps >= c.nt ? 1 : (c.nt + tps - 1) / tps;
+      const int mine = SPLITS ? nrb * ns : nrb, slots = nrb * ns;
+      int end = mine, send = slots;
+      for (int o = 1; o < m64; o <<= 1) {
+        const int u = __shfl_up(end, o), v = SPLITS ? u : __shfl_up(send, o);
+        if (lane >= o) {
+          end += u;
+          send += v;
         }
       }
-      who = __builtin_amdgcn_ds_permute(rank * 4, who);
-      c.nt = __builtin_amdgcn_ds_permute(rank * 4, c.nt);
-      c.nrb = __builtin_amdgcn_ds_permute(rank * 4, c.nrb);
+      const uint64_t m = __ballot(lane < m64 && base + end > x);
+      if (m != 0) {
+        const int l = __builtin_ctzll(m);
+        it.found = true;
+        it.b = __builtin_amdgcn_readlane(who, l);
+        const int at = x - base - __builtin_amdgcn_readlane(end - mine, l);
+        it.ns = __builtin_amdgcn_readlane(ns, l);
+        const int block = SPLITS ? at / it.ns : at;
+        it.s = SPLITS ? at % it.ns : 0;
+        it.slot = slot + __builtin_amdgcn_readlane(send - slots, l) + block * it.ns + it.s;
+        it.rb = w.longest_first ? __builtin_amdgcn_readlane(nrb, l) - 1 - block : block;
+        break;
+      }
+      base += __builtin_amdgcn_readlane(end, m64 - 1);
+      slot += __builtin_amdgcn_readlane(send, m64 - 1);
     }
-    const int nrb = c.nrb, ns = tps >= c.nt ? 1 : (c.nt + tps - 1) / tps;
-    const int mine = SPLITS ? nrb * ns : nrb, slots = nrb * ns;
-    int end = mine, send = slots;
-    for (int o = 1; o < m64; o <<= 1) {
-      const int u = __shfl_up(end, o), v = SPLITS ? u : __shfl_up(send, o);
-      if (lane >= o) {
-        end += u;
-        send += v;
+    if (it.found) {
+      it.seq = seq_of(a, it.b, w.causal);
+      it.seq.ok = it.seq.ok && it.seq.n <= w.max_q;
+    }
+    return it;
+  }
+};
+
+// An item that wave 0 has found, for the whole workgroup (barriers on both sides).
+constexpr int kItemInts = 12;
+template <class F>
+__device__ __forceinline__ RowItem shared_item(int* lds, F&& find) {
+  __syncthreads();  // the last item's LDS is free
+  if (threadIdx.x < 64) {
+    const RowItem it = find();
+    if (threadIdx.x == 0) {
+      lds[0] = it.found;
+      if (it.found) {
+        lds[1] = it.b;
+        lds[2] = it.rb;
+        lds[3] = it.s;
+        lds[4] = it.ns;
+        lds[5] = it.slot;
+        lds[6] = it.seq.q0;
+        lds[7] = it.seq.n;
+        lds[8] = it.seq.len;
+        lds[9] = it.seq.ok;
       }
     }
-    const uint64_t m = __ballot(lane < m64 && base + end > x);
-    if (m != 0) {
-      const int l = __builtin_ctzll(m);
-      it.found = true;
-      it.b = __builtin_amdgcn_readlane(who, l);
-      const int at = __builtin_amdgcn_readfirstlane(x - base - __shfl(end - mine, l));
-      it.ns = __builtin_amdgcn_readfirstlane(__shfl(ns, l));
-      const int block = SPLITS ? at / it.ns : at;
-      it.s = SPLITS ? at % it.ns : 0;
-      it.slot = __builtin_amdgcn_readfirstlane(slot + __shfl(send - slots, l)) + block * it.ns + it.s;
-      it.rb = w.longest_first ? __builtin_amdgcn_readlane(nrb, l) - 1 - block : block;
-      break;
-    }
-    base += __shfl(end, m64 - 1);
-    slot += __shfl(send, m64 - 1);
   }
-  if (it.found) {
-    it.seq = seq_of(a, it.b, w.causal);
-    it.seq.ok = it.seq.ok && it.seq.n <= w.max_q;
-  }
+  __syncthreads();
+  auto get = [lds](int i) { return __builtin_amdgcn_readfirstlane(lds[i]); };
+  RowItem it;
+  it.found = get(0) != 0;
+  it.b = get(1);
+  it.rb = get(2);
+  it.s = get(3);
+  it.ns = get(4);
+  it.slot = get(5);
+  it.seq.q0 = get(6);
+  it.seq.n = get(7);
+  it.seq.len = get(8);
+  it.seq.ok = get(9) != 0;
   return it;
 }
 
@@ -236,6 +289,15 @@ __device__ float exact_joint(const PagedArgs& a, const bf16* qrow, int b, int g,
 __device__ __forceinline__ float max8(const float (&x)[8]) {  // three v_max3 and one v_max
   return fmaxf(fmaxf(fmaxf(fmaxf(fmaxf(x[0], x[1]), x[2]), fmaxf(fmaxf(x[3], x[4]), x[5])), x[6]),
                x[7]);
+}
+
+// max(x over the lanes with the same l16), by lane swaps.
+__device__ __forceinline__ float max_groups(float x) {
+  unsigned u = __float_as_uint(x);
+  const auto a = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+  u = __float_as_uint(fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1])));
+  const auto b = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
 
 // ---- the read -------------------------------------------------------------------
@@ -431,8 +493,7 @@ struct RowRead {
       if (__any(exponents() > kRowBias + kLag)) {
         float mx = fmaxf(fmaxf(fmaxf(s[rb][0][0], s[rb][0][1]), fmaxf(s[rb][0][2], s[rb][0][3])),
                          fmaxf(fmaxf(s[rb][1][0], s[rb][1][1]), fmaxf(s[rb][1][2], s[rb][1][3])));
-        mx = fmaxf(mx, __shfl_xor(mx, 16));
-        mx = fmaxf(mx, __shfl_xor(mx, 32)) * scale2;
+        mx = max_groups(mx) * scale2;
         const float mn = mx > m[rb] + kLag ? mx : m[rb];
         const float f = mn == m[rb] ? 1.f : exp2_hw(m[rb] - mn);
         m[rb] = mn;
@@ -482,9 +543,7 @@ struct RowRead {
         return max8(x);
       };
       if (__any(exponents() > kRowBias + kLag)) {
-        float mx = max8(v);
-        mx = fmaxf(mx, __shfl_xor(mx, 16));
-        mx = fmaxf(mx, __shfl_xor(mx, 32)) * bl[cb];
+        const float mx = max_groups(max8(v)) * bl[cb];
         const float cn = mx > c[cb] + kLag ? mx : c[cb];
         const float f = cn == c[cb] ? 1.f : exp2_hw(c[cb] - cn);
         c[cb] = cn;
@@ -538,7 +597,7 @@ struct ReadArgs {
   const float* beta;   // [heads][DV]
   void* out;           // [ntok][H][DV] float32 or bf16
   int* tps;            // [2] tiles of a split, as the two kernels have chosen them
-  float* part;         // [slot][rps][DV + 1]: log2 joint sums, then the row's log2 normaliser
+  float* part;         // [slot][rps][part_row]: log2 joint sums, the row's log2 normaliser
   float* wide_part;    // of the wide kernel
   int H, G;            // query heads, of a cached head
   int rps, wide_rps;   // rows of a slot
@@ -550,6 +609,20 @@ struct ReadArgs {
 
 __host__ __device__ __forceinline__ Work rows_work(const PagedArgs& a, const ReadArgs& r) {
   return Work{r.G, kRowsMax, kRowTile, 0, r.most_rows, a.max_q, r.causal != 0, false};
+}
+
+// A row of partial results: its channels' sums, its normaliser, and room to keep the
+// next row aligned for loads of four.
+__host__ __device__ constexpr int part_row(int dv) { return dv + 4; }
+
+__device__ __forceinline__ void put4(const ReadArgs& r, size_t at, f32x4 x) {
+  if (r.obf16) {
+    const bf16x2 a = to_bf16x2(x[0], x[1]), b = to_bf16x2(x[2], x[3]);
+    *reinterpret_cast<u32x2v*>(static_cast<bf16*>(r.out) + at) =
+        u32x2v{__builtin_bit_cast(unsigned, a), __builtin_bit_cast(unsigned, b)};
+  } else {
+    *reinterpret_cast<f32x4*>(static_cast<float*>(r.out) + at) = x;
+  }
 }
 
 __device__ __forceinline__ void put(const ReadArgs& r, size_t at, float x) {
@@ -581,10 +654,7 @@ __device__ __forceinline__ void rows_body(const PagedArgs& a, const ReadArgs& r,
   const float scale2 = kLog2e / sqrtf((float)DK);
 
   int t = tb + wave;
-  if (t < te) {
-    w.load_pages(t);
-    w.load(t, 0);
-  }
+  if (t < te) w.load_pages(t);
   int lim[RB];
 #pragma unroll
   for (int rb = 0; rb < RB; ++rb) {
@@ -608,6 +678,7 @@ __device__ __forceinline__ void rows_body(const PagedArgs& a, const ReadArgs& r,
     w.c[cb] = kNone;
     if (__any(!(b >= kLoBelow))) w.lo_blocks |= 1u << cb;
   }
+  if (t < te) w.load(t, 0);
   for (int n = 1; t < te; t += NW, n = (n + 1) & 31) {
     const int k0 = t * kRowTile, next = t + NW;
     if (n == 0 && next < te) w.load_pages(next);
@@ -618,7 +689,10 @@ __device__ __forceinline__ void rows_body(const PagedArgs& a, const ReadArgs& r,
   float* const fm = reinterpret_cast<float*>(smem + NW * C::AREA);  // [NW][32] row maxima
   float* const fl = fm + NW * kRowsMax;                            // [NW][32] row sums
   float* const fc = fl + NW * kRowsMax;                            // [NW][DV] shifts
-  int* const fbad = reinterpret_cast<int*>(fc + NW * DV);           // [NW]
+  float* const rm = fc + NW * DV;                                  // [32] a row's M
+  float* const rl = rm + kRowsMax;                                 // [32] and its sum there
+  float* const ct = rl + kRowsMax;                                 // [DV] a channel's Cc
+  int* const fbad = reinterpret_cast<int*>(ct + DV);               // [NW]
 #pragma unroll
   for (int rb = 0; rb < RB; ++rb) {
     if (w.grp == 0) fm[wave * kRowsMax + rb * 16 + w.l16] = w.m[rb];
@@ -643,6 +717,16 @@ __device__ __forceinline__ void rows_body(const PagedArgs& a, const ReadArgs& r,
     for (int x = 1; x < NW; ++x) t = fmaxf(t, p[x * stride]);
     return t;
   };
+  // (for all to read after the next barrier)
+  if (tid < 16 * RB) {
+    const float M = top_of(fm + tid, kRowsMax);
+    float l = 0.f;
+#pragma unroll
+    for (int x = 0; x < NW; ++x) l += fl[x * kRowsMax + tid] * exp2_hw(fm[x * kRowsMax + tid] - M);
+    rm[tid] = M;
+    rl[tid] = l;
+  }
+  if (tid >= 64 * NW - DV) ct[tid - (64 * NW - DV)] = top_of(fc + tid - (64 * NW - DV), DV);
   float cf[C::NCB];
 #pragma unroll
   for (int cb = 0; cb < C::NCB; ++cb) {
@@ -671,13 +755,11 @@ __device__ __forceinline__ void rows_body(const PagedArgs& a, const ReadArgs& r,
       const int q = e / DV, j = e % DV, row = r0 + rb * 16 + q;
       if (rb * 16 + (e & ~63) / DV >= nr) break;  // the wave's rows are past the last
       const bool live = rb * 16 + q < nr;
-      const float M = top_of(fm + rb * 16 + q, kRowsMax), top = top_of(fc + j, DV);
-      float sum = 0.f, l = 0.f;
+      const float M = rm[rb * 16 + q], l = rl[rb * 16 + q], top = ct[j];
+      float sum = 0.f;
 #pragma unroll
-      for (int x = 0; x < NW; ++x) {
+      for (int x = 0; x < NW; ++x)
         sum += reinterpret_cast<const float*>(smem + x * C::AREA)[q * C::OROW + j];
-        l += fl[x * kRowsMax + rb * 16 + q] * exp2_hw(fm[x * kRowsMax + rb * 16 + q] - M);
-      }
       const float blj = r.beta[g * DV + j] * kLog2e;
       const int seen = min(kend, row_limit(sq, row, r.G, causal));  // of this range, up to here
       const bool none = !live || seen <= kbeg;
@@ -704,7 +786,7 @@ __device__ __forceinline__ void rows_body(const PagedArgs& a, const ReadArgs& r,
         if (bad) o = NAN;
         put(r, ((size_t)(sq.q0 + row / r.G) * r.H + g * r.G + row % r.G) * DV + j, o);
       } else {
-        float* p = r.part + ((size_t)slot * r.rps + rb * 16 + q) * (DV + 1);
+        float* p = r.part + ((size_t)slot * r.rps + rb * 16 + q) * part_row(DV);
         p[j] = bad ? NAN : y;
         if (j == 0) p[DV] = bad ? NAN : lp;
       }
@@ -729,23 +811,29 @@ __device__ __forceinline__ void all_nan(const ReadArgs& r, const RowItem& it, in
 // Workgroup i takes the pieces i, i + gridDim, ...: piece x * heads + g is item x
 // of cached head g.  RB = 1: no sequence has more than 16 rows.
 template <int DK, int DV, int KV, int RB, int NW>
-__global__ __launch_bounds__(64 * NW, NW == kRowWaves ? row_waves(DK, DV, KV, RB) : 2)
+__global__ __launch_bounds__(64 * NW, 2)
 void paged_rows_kernel(PagedArgs a, ReadArgs r) {
   using C = RowCfg<DK, DV>;
   __shared__ __align__(16) unsigned char
-      smem[NW * (C::AREA + (2 * kRowsMax + DV) * 4 + 4)];
+      smem[NW * (C::AREA + (2 * kRowsMax + DV) * 4 + 4) + (2 * kRowsMax + DV) * 4];
+  __shared__ int item[kItemInts];
   const Work wk = rows_work(a, r);
-  const int tps = tiles_per_split(a, wk, r.target);
-  if (r.target != 0 && blockIdx.x == 0 && threadIdx.x == 0) r.tps[0] = tps;
+  int tps = 0;  // (wave 0's)
   for (int piece = blockIdx.x;; piece += gridDim.x) {
     const int g = piece % a.heads;
-    const RowItem it = find_item<true>(a, wk, tps, piece / a.heads);
+    const RowItem it = shared_item(item, [&] {
+      const Planner plan(a, wk);
+      if (tps == 0) {
+        tps = plan.tiles_per_split(r.target, kRowWaves);
+        if (r.target != 0 && blockIdx.x == 0 && threadIdx.x == 0) r.tps[0] = tps;
+      }
+      return plan.template find<true>(tps, piece / a.heads);
+    });
     if (!it.found) return;
     if (!it.seq.ok || it.seq.len == 0) {
       all_nan<DV>(r, it, g, kRowsMax, 64 * NW);
       continue;
     }
-    __syncthreads();  // the last piece's LDS is free
     const long long left = (long long)it.seq.n * r.G - (long long)it.rb * kRowsMax;
     if (RB == 1 || left <= 16) rows_body<DK, DV, KV, 1, NW>(a, r, it, g, piece, smem);
     else rows_body<DK, DV, KV, 2, NW>(a, r, it, g, piece, smem);
@@ -774,18 +862,20 @@ struct MergePart {
   int rps, rows, groups;  // rows of a slot, of a chunk; workgroups
 };
 
-constexpr int kMergeThreads = 512;
-constexpr int kMergeBatch = 4;
+constexpr int kMergeThreads = 256;
+constexpr int kMergeBatch = 8;
 
 // Workgroup (chunk of a row block, cached head); the first p.groups of them for p,
-// the others for o.  The threads are groups of DV; a row's splits are shared by so
-// many groups (a power of two) that each takes one batch of them, if there are
-// enough, and the groups meet in LDS.
+// the others for o.  A thread has four channels of a row; a row's splits are shared
+// by so many threads (a power of two) that each takes one batch of them, if there
+// are enough, and these meet in LDS.
 template <int DV>
 __global__ __launch_bounds__(kMergeThreads) void paged_merge_kernel(PagedArgs a, ReadArgs r,
                                                                     MergePart p, MergePart o) {
-  constexpr int NG = kMergeThreads / DV;
-  __shared__ float4 meet[NG][DV];
+  constexpr int TPR = DV / 4, NG = kMergeThreads / TPR;  // threads of a row, groups of them
+  __shared__ f32x4 meet_m[NG][TPR], meet_s[NG][TPR];
+  __shared__ float meet_d[NG][2];
+  __shared__ int item[kItemInts];
   const bool second = (int)blockIdx.x >= p.groups;
   const MergePart& x = second ? o : p;
   const int tps = *x.tps;
@@ -793,57 +883,91 @@ __global__ __launch_bounds__(kMergeThreads) void paged_merge_kernel(PagedArgs a,
   const int id = second ? blockIdx.x - p.groups : blockIdx.x;
   const int chunks = (min(x.w.br, x.rps) + x.rows - 1) / x.rows;  // of a row block
   const int g = id % a.heads, xc = id / a.heads;
-  const RowItem it = find_item<false>(a, x.w, tps, xc / chunks);
+  const RowItem it = shared_item(item, [&] {
+    return Planner(a, x.w).template find<false>(tps, xc / chunks);
+  });
   if (!it.found || it.ns == 1) return;
   const int c0 = xc % chunks * x.rows;  // first row of the block that is merged here
   const int r0 = it.rb * x.w.br + c0;
   const int nr = (int)min((long long)it.seq.n * r.G - r0, (long long)x.rows);
   if (nr <= 0) return;
   int per = 1;  // groups of a row
-  while (per < NG && (per * kMergeBatch < it.ns || NG / per > nr)) per <<= 1;
-  const int rows = NG / per, grp = threadIdx.x / DV, j = threadIdx.x % DV, sub = grp % per;
-  const float blj = r.beta[g * DV + j] * kLog2e;
-  // 2^x / 2^x of a partial sum's logarithm: 0 of none, NaN of NaN
-  auto one = [](float y) { return y == -INFINITY ? 0.f : y != y ? y : 1.f; };
-  const size_t step = (size_t)a.heads * x.rps * (DV + 1);  // from split to split
-  const float* base = x.part + ((size_t)((size_t)it.slot * a.heads + g) * x.rps + c0) * (DV + 1);
+  while (per < NG && per * kMergeBatch < it.ns) per <<= 1;
+  const int rows = NG / per, grp = threadIdx.x / TPR, c = threadIdx.x % TPR, sub = grp % per;
+  const f32x4 bl = *reinterpret_cast<const f32x4*>(r.beta + g * DV + c * 4) * kLog2e;
+  constexpr int PR = part_row(DV);
+  const size_t step = (size_t)a.heads * x.rps * PR;  // from split to split
+  const float* base = x.part + ((size_t)((size_t)it.slot * a.heads + g) * x.rps + c0) * PR;
+  const f32x4 kNone4 = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
   for (int q0 = 0; q0 < nr; q0 += rows) {
     const int q = q0 + grp / per;
-    float M = -INFINITY, S = 0.f, md = -INFINITY, sd = 0.f;
+    f32x4 M = kNone4, S = {0.f, 0.f, 0.f, 0.f};
+    float md = -INFINITY, sd = 0.f;
     if (q < nr) {
-      const float* pq = base + (size_t)q * (DV + 1);
+      const float* pq = base + (size_t)q * PR;
       for (int s0 = sub; s0 < it.ns; s0 += kMergeBatch * per) {
-        float y[kMergeBatch], d[kMergeBatch];
+        f32x4 y[kMergeBatch];
+        float d[kMergeBatch];
 #pragma unroll
         for (int u = 0; u < kMergeBatch; ++u) {
           const int s = s0 + u * per;
           const float* ps = pq + step * min(s, it.ns - 1);
-          y[u] = s < it.ns ? ps[j] : -INFINITY;
-          d[u] = s < it.ns ? ps[DV] : -INFINITY;
+          y[u] = *reinterpret_cast<const f32x4*>(ps + c * 4);
+          d[u] = ps[DV];
+          if (s >= it.ns) {
+            y[u] = kNone4;
+            d[u] = -INFINITY;
+          }
         }
+        // the batch's maximum first: its exponentials then wait for nothing else
+        auto fold = [&](float& m, float& z, auto&& at) {
+          float top = at(0), sum = 0.f;
 #pragma unroll
-        for (int u = 0; u < kMergeBatch; ++u) {
-          lse_join(M, S, y[u], one(y[u]));
-          lse_join(md, sd, d[u], one(d[u]));
+          for (int u = 1; u < kMergeBatch; ++u) top = fmaxf(top, at(u));
+          const float ref = fmaxf(top, -3e38f);  // none of the batch: zeros, or NaN
+#pragma unroll
+          for (int u = 0; u < kMergeBatch; ++u) sum += exp2_hw(at(u) - ref);
+          lse_join(m, z, top, sum);
+        };
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          float m = M[e], z = S[e];
+          fold(m, z, [&](int u) { return y[u][e]; });
+          M[e] = m;
+          S[e] = z;
         }
+        fold(md, sd, [&](int u) { return d[u]; });
       }
     }
     if (per > 1) {  // the same for the whole workgroup
       if (q0 > 0) __syncthreads();
-      meet[grp][j] = make_float4(M, S, md, sd);
+      meet_m[grp][c] = M;
+      meet_s[grp][c] = S;
+      if (c == 0) {
+        meet_d[grp][0] = md;
+        meet_d[grp][1] = sd;
+      }
       __syncthreads();
       if (sub == 0) {
         for (int u = 1; u < per; ++u) {
-          const float4 z = meet[grp + u][j];
-          lse_join(M, S, z.x, z.y);
-          lse_join(md, sd, z.z, z.w);
+          const f32x4 m2 = meet_m[grp + u][c], s2 = meet_s[grp + u][c];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            float m = M[e], z = S[e];
+            lse_join(m, z, m2[e], s2[e]);
+            M[e] = m;
+            S[e] = z;
+          }
+          lse_join(md, sd, meet_d[grp + u][0], meet_d[grp + u][1]);
         }
       }
     }
     if (q < nr && sub == 0) {
-      const float f = ((M - md) + (log2_hw(S) - log2_hw(sd))) / blj;
+      f32x4 f;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) f[e] = ((M[e] - md) + (log2_hw(S[e]) - log2_hw(sd))) / bl[e];
       const int row = r0 + q;
-      put(r, ((size_t)(it.seq.q0 + row / r.G) * r.H + g * r.G + row % r.G) * DV + j, f);
+      put4(r, ((size_t)(it.seq.q0 + row / r.G) * r.H + g * r.G + row % r.G) * DV + c * 4, f);
     }
   }
 }

@@ -42,7 +42,7 @@ struct WideLds {
   static constexpr size_t OFF_RAW = (C::LDS + 15) / 16 * 16;
   static constexpr size_t OFF_BAD = OFF_RAW + (MX ? C::NW * (RAWK + RAWV) : 0);
   static constexpr size_t BYTES = OFF_BAD + 16;
-  static_assert(BYTES <= 160 * 1024, "LDS budget");
+  static_assert(BYTES + kItemInts * 4 <= 160 * 1024, "LDS budget");
 };
 
 // Lane offset, inside the 16 rows that a pair of waves fills, of the 16-byte slot
@@ -85,8 +85,8 @@ __device__ __forceinline__ void wide_body(const PagedArgs& a, const ReadArgs& r,
   const int te = (int)((long long)(it.s + 1) * all / it.ns);
   const int ntiles = te - tb;
   if (ntiles <= 0) {  // an early block of a sequence has fewer tiles than splits
-    float* p = r.wide_part + (size_t)slot_id * r.wide_rps * (C::DV + 1);
-    for (int e = tid; e < nr * (C::DV + 1); e += C::NT) p[e] = -INFINITY;
+    float* p = r.wide_part + (size_t)slot_id * r.wide_rps * part_row(C::DV);
+    for (int e = tid; e < nr * part_row(C::DV); e += C::NT) p[e] = -INFINITY;
     return;
   }
 
@@ -442,15 +442,14 @@ __device__ __forceinline__ void wide_body(const PagedArgs& a, const ReadArgs& r,
   constexpr int LPR = C::DV / 4, RPI = 64 / LPR;
   const int c4 = (lane % LPR) * 4;
   if (!single) {
-    float* p = r.wide_part + ((size_t)slot_id * r.wide_rps + wr0) * (C::DV + 1);
-    if (hl == 0 && mine) p[n * (C::DV + 1) + C::DV] = bad ? __builtin_nanf("") : lp;
+    constexpr int PR = part_row(C::DV);
+    float* p = r.wide_part + ((size_t)slot_id * r.wide_rps + wr0) * PR;
+    if (hl == 0 && mine) p[n * PR + C::DV] = bad ? __builtin_nanf("") : lp;
 #pragma unroll 4
     for (int q = 0; q < 32; q += RPI) {
       const int rr = q + lane / LPR;
       const f32x4 o = *reinterpret_cast<const f32x4*>(stage + rr * SROW + c4);
-      if (wr0 + rr >= nr) continue;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) p[rr * (C::DV + 1) + c4 + e] = o[e];
+      if (wr0 + rr < nr) *reinterpret_cast<f32x4*>(p + rr * PR + c4) = o;
     }
     return;
   }
@@ -459,15 +458,7 @@ __device__ __forceinline__ void wide_body(const PagedArgs& a, const ReadArgs& r,
     const int rr = q + lane / LPR, x = r0 + wr0 + rr;
     const f32x4 o = *reinterpret_cast<const f32x4*>(stage + rr * SROW + c4);
     if (wr0 + rr >= nr) continue;
-    const size_t at =
-        ((size_t)(sq.q0 + x / r.G) * r.H + g * r.G + x % r.G) * C::DV + c4;
-    if (r.obf16) {
-      const bf16x2 o01 = to_bf16x2(o[0], o[1]), o23 = to_bf16x2(o[2], o[3]);
-      const u32x2 ob = {__builtin_bit_cast(unsigned, o01), __builtin_bit_cast(unsigned, o23)};
-      *reinterpret_cast<u32x2*>(static_cast<bf16*>(r.out) + at) = ob;
-    } else {
-      *reinterpret_cast<f32x4*>(static_cast<float*>(r.out) + at) = o;
-    }
+    put4(r, ((size_t)(sq.q0 + x / r.G) * r.H + g * r.G + x % r.G) * C::DV + c4, o);
   }
 }
 
@@ -489,28 +480,22 @@ __host__ __device__ __forceinline__ Work wide_work(const PagedArgs& a, const Rea
 }
 
 constexpr int kWideUnits = 256;  // compute units, which hold one workgroup each
+constexpr int kMostSplitBlocks = kWideUnits / 2;
 constexpr int kSplitCost = 8;    // a split's store and its part of the merge, in tiles
 constexpr int kLeastTiles = 4;   // of a split
 
 // Tiles of a split of the wide kernel.  Where the row blocks leave at least half of
 // the compute units idle, the smallest with which all splits still have a unit each,
 // if that saves more tiles than the splits cost.
-__device__ __forceinline__ int wide_tiles(const PagedArgs& a, const ReadArgs& r, const Work& w) {
+__device__ __forceinline__ int wide_tiles(const Planner& plan, const ReadArgs& r) {
   if (!r.split_wide) return kWhole;
   const auto count = [&](int tps) {
-    return sum_items(a, w, [=](const RowCounts& c) {
-             return (long long)c.nrb * ((c.nt + (long long)tps - 1) / tps);
-           }) * a.heads;
+    return plan.total(
+        [=](const RowCounts& c) { return (long long)c.nrb * ((c.nt + (long long)tps - 1) / tps); });
   };
   const long long items = count(kWhole);
-  if (items == 0 || items * 2 > kWideUnits) return kWhole;
-  int longest = 0;
-  for (int b0 = 0; b0 < a.nseq; b0 += 64) {
-    const int b = b0 + (threadIdx.x & 63);
-    if (b < a.nseq) longest = max(longest, row_counts(seq_of(a, b, w.causal), w).nt);
-  }
-  for (int o = 32; o > 0; o >>= 1) longest = max(longest, __shfl_xor(longest, o));
-  longest = __builtin_amdgcn_readfirstlane(longest);
+  if (items == 0 || items > kMostSplitBlocks) return kWhole;
+  const int longest = plan.longest();
   int lo = kLeastTiles, hi = longest;  // the smallest that fits is in lo .. hi
   while (lo < hi) {
     const int mid = (lo + hi) >> 1;
@@ -528,11 +513,15 @@ __global__ __launch_bounds__(512) void paged_wide_kernel(PagedArgs a, ReadArgs r
   using C2 = Cfg<DK, DV, 8, kFem, true, false, 2>;
   static_assert(WideLds<C1, KV>::BYTES == WideLds<C2, KV>::BYTES, "one LDS layout");
   __shared__ __align__(16) unsigned char smem[WideLds<C1, KV>::BYTES];
+  __shared__ int item[kItemInts];
   const Work w = wide_work(a, r);
-  const int tps = wide_tiles(a, r, w);
-  if (r.split_wide && blockIdx.x == 0 && threadIdx.x == 0) r.tps[1] = tps;
   const int g = blockIdx.x % a.heads;
-  const RowItem it = find_item<true>(a, w, tps, blockIdx.x / a.heads);
+  const RowItem it = shared_item(item, [&] {
+    const Planner plan(a, w);
+    const int tps = wide_tiles(plan, r);
+    if (r.split_wide && blockIdx.x == 0 && threadIdx.x == 0) r.tps[1] = tps;
+    return plan.template find<true>(tps, blockIdx.x / a.heads);
+  });
   if (!it.found) return;
   if (!it.seq.ok || it.seq.len == 0) {
     all_nan<DV>(r, it, g, kWideRows, 512);
