@@ -98,8 +98,8 @@ hipError_t launch_cache_gather(const PagedArgs& a, int kv, int dk, int dv, void*
 
 // The launches of a read: how many workgroups, and the scratch they need.
 struct PagedPlan {
-  bool rows, wide;         // whether the kernel for few rows runs, and the one for many
-  long long most_rows;     // sequences of the first: rows <= most_rows, of the second:
+  bool rows, wide;         // whether sequences of few rows may be there, and of many
+  long long most_rows;     // sequences of few rows: rows <= most_rows, of many:
   long long wide_least;    //   rows > wide_least
   int row_blocks, target;  // few rows: bound of the row blocks of a cached head, and of
                            //   the splits over all heads (0: nothing is split)

@@ -16,8 +16,8 @@ constexpr int kMergeRows = 8;    // of a merge's workgroup, few rows a block
 
 // Rows of a merge's workgroup, many rows a block: as many as leave about four
 // workgroups a compute unit, whose cost is mostly finding their rows (one block of
-// 256 rows and eight heads in 32 splits: 51 us with 8 rows, 59 with 16; ten blocks
-// and twelve heads in two: 64 and 58).
+// 256 rows and eight heads in 32 splits: 48 us with 4 rows, 51 with 8, 59 with 16;
+// ten blocks and twelve heads in two: 64 with 8 and 58 with 16).
 int wide_merge_rows(size_t rows) {
   int n = 4;
   while (n < 16 && rows / (2 * n) >= 4 * kUnits) n *= 2;
@@ -42,13 +42,13 @@ PagedPlan paged_plan(const PagedArgs& a, int H, int dv) {
   p.wide_least = p.rows ? kRowsMax : 0;
   size_t at = 256;  // the two kernels' split sizes
   p.part_at = at;
-  if (p.rows) {
+  if (p.rows) {  // in a launch of their own, or in the other kernel's
     const long long m = std::min<long long>(most, kRowsMax);
     p.row_blocks = blocks(m, kRowsMax);
     p.rps = (int)m;
     const bool brief = keys <= kShortKeys;
     p.waves = brief ? 2 * kRowWaves : kRowWaves;
-    const int room = kUnits * (brief ? 1 : kRowGroups);
+    const int room = kUnits * (brief || p.wide ? 1 : kRowGroups);
     p.target = brief ? 0 : room;
     p.groups = p.target ? room : std::min<size_t>((size_t)p.row_blocks * a.heads, room);
     if (p.target) at += up256((size_t)p.target * p.rps * part_row(dv) * sizeof(float));
@@ -64,6 +64,8 @@ PagedPlan paged_plan(const PagedArgs& a, int H, int dv) {
       at += up256((size_t)kWideUnits * p.wide_rps * part_row(dv) * sizeof(float));
     }
   }
+  if (p.wide && p.rows)
+    p.wide_groups += std::max<size_t>((size_t)p.row_blocks * a.heads, p.target);
   p.ws_bytes = p.target || p.split_wide ? at : 0;
   return p;
 }
@@ -85,27 +87,29 @@ hipError_t launch_paged_read(const PagedArgs& a, const PagedPlan& plan, int kv, 
   r.wide_rps = plan.wide_rps;
   r.target = plan.target;
   r.split_wide = plan.split_wide;
+  r.rows_too = plan.wide && plan.rows;
   r.most_rows = plan.most_rows;
   r.wide_least = plan.wide_least;
   r.causal = causal;
   r.obf16 = obf16;
   // The merge's workgroups: calls of more blocks than splits are aimed at are not split.
   MergePart few = {}, many = {};
-  if (plan.rows && plan.target) {
-    few = MergePart{rows_work(a, r), r.tps, r.part, plan.rps, kMergeRows, 0};
-    const size_t blocks = std::min<size_t>((size_t)plan.row_blocks * a.heads, plan.target);
-    few.groups = (int)(blocks * ((plan.rps + kMergeRows - 1) / kMergeRows));
-  }
+  auto part = [&](MergePart& m, const Work& w, const int* tps, const float* at, int rps,
+                  size_t blocks, int rows) {
+    m = MergePart{w, tps, at, rps, rows, 0};
+    m.groups = (int)(blocks * ((rps + m.rows - 1) / m.rows));
+  };
+  if (plan.rows && plan.target)
+    part(few, rows_work(a, r), r.tps, r.part, plan.rps,
+         std::min<size_t>((size_t)plan.row_blocks * a.heads, plan.target), kMergeRows);
   if (plan.wide && plan.split_wide) {
     const size_t blocks = std::min<size_t>((size_t)plan.wide_blocks * a.heads, kMostSplitBlocks);
-    const int n = wide_merge_rows(blocks * plan.wide_rps);
-    many = MergePart{wide_work(a, r), r.tps + 1, r.wide_part, plan.wide_rps, n, 0};
-    many.groups = (int)(blocks * ((plan.wide_rps + n - 1) / n));
+    part(many, wide_work(a, r), r.tps + 1, r.wide_part, plan.wide_rps, blocks,
+         wide_merge_rows(blocks * plan.wide_rps));
   }
   auto go = [&](auto rows, auto wide, auto merge) {
     hipError_t e = hipSuccess;
-    if (plan.wide) e = wide(a, r, plan, kv, stream);
-    if (e == hipSuccess && plan.rows) e = rows(a, r, plan, kv, stream);
+    e = plan.wide ? wide(a, r, plan, kv, stream) : rows(a, r, plan, kv, stream);
     if (e == hipSuccess && few.groups + many.groups > 0) {
       hipLaunchKernelGGL(merge, dim3((unsigned)(few.groups + many.groups)), dim3(kMergeThreads), 0,
                          stream, a, r, few, many);

@@ -47,6 +47,7 @@ namespace fem {
 constexpr int kRowGroups = 2;
 
 constexpr int kRowsMax = 32;       // query rows of a block
+constexpr int kRowLeast = 8;       // tiles of a split at least, two a wave
 constexpr int kRowTile = 32;       // keys of a wave's tile
 constexpr int kRowWaves = 4;       // of a workgroup; calls with short contexts take twice as
                                    // many and do not split (kShortKeys)
@@ -72,7 +73,8 @@ struct Work {
 // A workgroup's piece of the work.
 struct RowItem {
   int b, rb, s, ns;  // sequence, row block, split and the number of splits
-  int slot;          // number of split s among those of one head
+  int slot;          // number of split s among those of one head (not found: of all splits)
+  int wide;          // of the wide kernel's own items
   Seq seq;
   bool found;
 };
@@ -162,6 +164,7 @@ struct Planner {
   __device__ __forceinline__ RowItem find(int tps, int x) const {
     RowItem it;
     it.found = false;
+    it.wide = 0;
     int base = 0, slot = 0;
     for (int b0 = 0; b0 < a.nseq; b0 += 64) {
       RowCounts c = counts(b0);
@@ -209,6 +212,8 @@ struct Planner {
     if (it.found) {
       it.seq = seq_of(a, it.b, w.causal);
       it.seq.ok = it.seq.ok && it.seq.n <= w.max_q;
+    } else {
+      it.slot = slot;
     }
     return it;
   }
@@ -233,6 +238,7 @@ __device__ __forceinline__ RowItem shared_item(int* lds, F&& find) {
         lds[7] = it.seq.n;
         lds[8] = it.seq.len;
         lds[9] = it.seq.ok;
+        lds[10] = it.wide;
       }
     }
   }
@@ -249,6 +255,7 @@ __device__ __forceinline__ RowItem shared_item(int* lds, F&& find) {
   it.seq.n = get(7);
   it.seq.len = get(8);
   it.seq.ok = get(9) != 0;
+  it.wide = get(10);
   return it;
 }
 
@@ -603,6 +610,7 @@ struct ReadArgs {
   int rps, wide_rps;   // rows of a slot
   int target;          // see tiles_per_split
   int split_wide;      // whether the wide kernel may split
+  int rows_too;        // whether it takes the sequences of few rows too
   long long most_rows, wide_least;  // the kernels' sequences: rows <= most, rows > least
   int causal, obf16;
 };
@@ -628,6 +636,12 @@ __device__ __forceinline__ void put4(const ReadArgs& r, size_t at, f32x4 x) {
 __device__ __forceinline__ void put(const ReadArgs& r, size_t at, float x) {
   if (r.obf16) static_cast<bf16*>(r.out)[at] = (bf16)x;
   else static_cast<float*>(r.out)[at] = x;
+}
+
+// LDS of a workgroup of nw waves: their areas, and the tables in which they meet.
+template <int DK, int DV>
+constexpr int row_lds(int nw) {
+  return nw * (RowCfg<DK, DV>::AREA + (2 * kRowsMax + DV) * 4 + 4) + (2 * kRowsMax + DV) * 4;
 }
 
 // The read of one split of one row block (at most 16 RB rows) of cached head g.
@@ -813,9 +827,7 @@ __device__ __forceinline__ void all_nan(const ReadArgs& r, const RowItem& it, in
 template <int DK, int DV, int KV, int RB, int NW>
 __global__ __launch_bounds__(64 * NW, 2)
 void paged_rows_kernel(PagedArgs a, ReadArgs r) {
-  using C = RowCfg<DK, DV>;
-  __shared__ __align__(16) unsigned char
-      smem[NW * (C::AREA + (2 * kRowsMax + DV) * 4 + 4) + (2 * kRowsMax + DV) * 4];
+  __shared__ __align__(16) unsigned char smem[row_lds<DK, DV>(NW)];
   __shared__ int item[kItemInts];
   const Work wk = rows_work(a, r);
   int tps = 0;  // (wave 0's)
@@ -824,7 +836,7 @@ void paged_rows_kernel(PagedArgs a, ReadArgs r) {
     const RowItem it = shared_item(item, [&] {
       const Planner plan(a, wk);
       if (tps == 0) {
-        tps = plan.tiles_per_split(r.target, kRowWaves);
+        tps = plan.tiles_per_split(r.target, kRowLeast);
         if (r.target != 0 && blockIdx.x == 0 && threadIdx.x == 0) r.tps[0] = tps;
       }
       return plan.template find<true>(tps, piece / a.heads);
@@ -939,35 +951,39 @@ __global__ __launch_bounds__(kMergeThreads) void paged_merge_kernel(PagedArgs a,
         fold(md, sd, [&](int u) { return d[u]; });
       }
     }
-    if (per > 1) {  // the same for the whole workgroup
-      if (q0 > 0) __syncthreads();
-      meet_m[grp][c] = M;
-      meet_s[grp][c] = S;
-      if (c == 0) {
-        meet_d[grp][0] = md;
-        meet_d[grp][1] = sd;
-      }
-      __syncthreads();
-      if (sub == 0) {
-        for (int u = 1; u < per; ++u) {
-          const f32x4 m2 = meet_m[grp + u][c], s2 = meet_s[grp + u][c];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            float m = M[e], z = S[e];
-            lse_join(m, z, m2[e], s2[e]);
-            M[e] = m;
-            S[e] = z;
-          }
-          lse_join(md, sd, meet_d[grp + u][0], meet_d[grp + u][1]);
-        }
-      }
-    }
-    if (q < nr && sub == 0) {
+    const int row = r0 + q;
+    const size_t at = ((size_t)(it.seq.q0 + row / r.G) * r.H + g * r.G + row % r.G) * DV + c * 4;
+    if (per == 1) {  // the same for the whole workgroup
       f32x4 f;
 #pragma unroll
       for (int e = 0; e < 4; ++e) f[e] = ((M[e] - md) + (log2_hw(S[e]) - log2_hw(sd))) / bl[e];
-      const int row = r0 + q;
-      put4(r, ((size_t)(it.seq.q0 + row / r.G) * r.H + g * r.G + row % r.G) * DV + c * 4, f);
+      if (q < nr) put4(r, at, f);
+      continue;
+    }
+    if (q0 > 0) __syncthreads();
+    meet_m[grp][c] = M;
+    meet_s[grp][c] = S;
+    if (c == 0) {
+      meet_d[grp][0] = md;
+      meet_d[grp][1] = sd;
+    }
+    __syncthreads();
+    if (q >= nr) continue;
+    // the row's groups share its channels
+    const int g0 = grp - sub;
+    auto join = [&](auto&& max_of, auto&& sum_of, float& m, float& z) {
+      m = max_of(0);
+      for (int u = 1; u < per; ++u) m = fmaxf(m, max_of(u));
+      const float ref = fmaxf(m, -3e38f);
+      z = 0.f;
+      for (int u = 0; u < per; ++u) z += sum_of(u) * exp2_hw(max_of(u) - ref);
+    };
+    join([&](int u) { return meet_d[g0 + u][0]; }, [&](int u) { return meet_d[g0 + u][1]; }, md, sd);
+    for (int e = sub; e < 4; e += per) {
+      float m, z;
+      join([&](int u) { return reinterpret_cast<const float*>(&meet_m[g0 + u][c])[e]; },
+           [&](int u) { return reinterpret_cast<const float*>(&meet_s[g0 + u][c])[e]; }, m, z);
+      put(r, at + e, ((m - md) + (log2_hw(z) - log2_hw(sd))) / (r.beta[g * DV + c * 4 + e] * kLog2e));
     }
   }
 }

@@ -262,7 +262,10 @@ __device__ __forceinline__ void wide_body(const PagedArgs& a, const ReadArgs& r,
       if (w >= 0 && w < PV::LOADS) vload(w, rv, (k + 1) & 1);
     };
   };
-  // the end of iteration k: tile k + 1 is in LDS
+  // The end of iteration k: tile k + 1 is in LDS.  8-bit: its codes, loaded an
+  // iteration ago, become its rows here, where no operand is live (between the
+  // phases: 482 to 498 us for a batch of chunks and tokens), and tile k + 2's are
+  // sent for.
   auto arrived = [&](int k) {
     wait_vmem();
     if (MX && k + 1 < ntiles) {
@@ -506,30 +509,54 @@ __device__ __forceinline__ int wide_tiles(const Planner& plan, const ReadArgs& r
 }
 
 // Workgroup x * heads + g: item x of cached head g, the longest sequences' first.  A
-// block's last rows, if at most 128, take the form with two key groups.
+// block's last rows, if at most 128, take the form with two key groups.  In a call
+// that may have sequences of few rows too (r.rows_too), their splits follow, read as
+// paged_rows_kernel reads them but by eight waves: they fill the units that the last
+// wide items leave idle (twelve sequences of 1 to 700 tokens, of which two with one:
+// MIXED).
 template <int DK, int DV, int KV>
 __global__ __launch_bounds__(512) void paged_wide_kernel(PagedArgs a, ReadArgs r) {
   using C1 = Cfg<DK, DV, 8, kFem, true, false, 1>;
   using C2 = Cfg<DK, DV, 8, kFem, true, false, 2>;
   static_assert(WideLds<C1, KV>::BYTES == WideLds<C2, KV>::BYTES, "one LDS layout");
+  static_assert(row_lds<DK, DV>(8) <= WideLds<C1, KV>::BYTES, "few rows fit");
   __shared__ __align__(16) unsigned char smem[WideLds<C1, KV>::BYTES];
   __shared__ int item[kItemInts];
-  const Work w = wide_work(a, r);
-  const int g = blockIdx.x % a.heads;
+  const int g = blockIdx.x % a.heads, x = blockIdx.x / a.heads;
   const RowItem it = shared_item(item, [&] {
+    const Work w = wide_work(a, r);
     const Planner plan(a, w);
     const int tps = wide_tiles(plan, r);
-    if (r.split_wide && blockIdx.x == 0 && threadIdx.x == 0) r.tps[1] = tps;
-    return plan.template find<true>(tps, blockIdx.x / a.heads);
+    const bool first = blockIdx.x == 0;
+    if (r.split_wide && first && threadIdx.x == 0) r.tps[1] = tps;
+    RowItem i = plan.template find<true>(tps, x);
+    i.wide = 1;
+    if (r.rows_too && (first || !i.found)) {
+      const Work wr = rows_work(a, r);
+      const Planner rows(a, wr);
+      const int t = rows.tiles_per_split(r.target, kRowLeast);
+      if (r.target != 0 && first && threadIdx.x == 0) r.tps[0] = t;
+      if (!i.found) {
+        i = rows.template find<true>(t, x - i.slot);
+        i.wide = 0;
+      }
+    }
+    return i;
   });
   if (!it.found) return;
   if (!it.seq.ok || it.seq.len == 0) {
-    all_nan<DV>(r, it, g, kWideRows, 512);
+    all_nan<DV>(r, it, g, it.wide ? kWideRows : kRowsMax, 512);
     return;
   }
-  const long long nr = (long long)it.seq.n * r.G - (long long)it.rb * kWideRows;
+  const int br = it.wide ? kWideRows : kRowsMax;
+  const long long nr = (long long)it.seq.n * r.G - (long long)it.rb * br;
+  const int slot = it.slot * a.heads + g;
+  if (!it.wide) {
+    if (nr <= 16) rows_body<DK, DV, KV, 1, 8>(a, r, it, g, slot, smem);
+    else rows_body<DK, DV, KV, 2, 8>(a, r, it, g, slot, smem);
+    return;
+  }
   const int nneed = lo_channels<C1>(r.beta + g * DV, threadIdx.x & 63);
-  const int slot = (int)blockIdx.x;
   if (nr > kWideRows / 2) wide_nlo<C1, KV, 0>((nneed + 31) >> 5, a, r, it, g, slot, smem, nneed);
   else wide_nlo<C2, KV, 0>((nneed + 31) >> 5, a, r, it, g, slot, smem, nneed);
 }
