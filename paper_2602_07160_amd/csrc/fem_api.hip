@@ -275,6 +275,7 @@ extern "C" int fem_cache_append(const fem_paged_cache* cache, const fem_paged_ba
   if (!ld_ok(k_ld, (long long)a.heads * cache->d_qk) || !ld_ok(v_ld, (long long)a.heads * cache->d_v))
     return FEM_ERR_SHAPE;
   if (!aligned16(k) || !aligned16(v)) return FEM_ERR_ALIGN;
+  if ((unsigned long long)a.ntok * a.heads > kMostWorkgroups) return FEM_ERR_SHAPE;
   return from_hip(fem::launch_cache_append(a, cache->type, cache->d_qk, cache->d_v, cache->k,
                                            cache->v, cache->k_scale, cache->v_scale, k, k_ld, v,
                                            v_ld, stream));
