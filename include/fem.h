@@ -406,7 +406,7 @@ typedef struct {
   const int* lens;        /* [n_seq]                                           */
   const int* table;       /* [n_seq, table_len] page numbers; entries past a
                              sequence's last page are not read                 */
-  int n_seq, table_len;   /* n_seq <= 65535, table_len * page <= 2^30          */
+  int n_seq, table_len;   /* n_seq <= 65535, table_len * page <= 2^26          */
   int n_tok;              /* rows of the packed tensors                        */
   int max_q;              /* no sequence has more new tokens                   */
 } fem_paged_batch;

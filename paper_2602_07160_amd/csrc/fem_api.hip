@@ -67,7 +67,7 @@ int paged_args(const fem_paged_cache* c, const fem_paged_batch* s, bool tokens, 
   if ((unsigned long long)c->pages * c->heads > (1ull << 31) ||
       (unsigned long long)c->pages * c->heads * c->page > (1ull << 40) || c->heads > 65535 ||
       s->n_seq > 65535 || s->n_tok > (1 << 28) ||
-      (unsigned long long)s->table_len * c->page > (1ull << 30))
+      (unsigned long long)s->table_len * c->page > (1ull << 26))
     return FEM_ERR_SHAPE;
   if (!aligned16(c->k) || !aligned16(c->v)) return FEM_ERR_ALIGN;
   a->k = static_cast<const uint8_t*>(c->k);
@@ -313,6 +313,7 @@ extern "C" int fem_paged_fwd(const fem_paged_cache* cache, const fem_paged_batch
   if (!ld_ok(q_ld, (long long)H * cache->d_qk)) return FEM_ERR_SHAPE;
   if (!aligned16(q) || !aligned16(out)) return FEM_ERR_ALIGN;
   const fem::PagedPlan plan = fem::paged_plan(a, H, cache->d_v);
+  if (plan.wide_groups > kMostWorkgroups) return FEM_ERR_SHAPE;
   rc = check_ws(ws, ws_bytes, plan.ws_bytes);
   if (rc != FEM_OK) return rc;
   return from_hip(fem::launch_paged_read(a, plan, cache->type, cache->d_qk, cache->d_v, q, q_ld,

@@ -69,6 +69,12 @@ class Call:
                 p = int(table[b, n // page])
                 src.k[p, :, n % page:] = stale
                 src.v[p, :, n % page:] = stale
+            elif n % page:
+                p = int(table[b, n // page])
+                for x in (self.cache.k, self.cache.v):
+                    x.view(torch.uint8)[p, :, n % page:] = 0x7f
+                for x in (self.cache.k_scale, self.cache.v_scale):
+                    x[p, :, n % page:] = 255
         self.batch = fem.PagedBatch(*[torch.from_numpy(x.copy()).cuda() for x in
                                       (self.starts, np.asarray(lens, np.int32), table)],
                                     n_tok=N, max_q=max(max(news), 1))
@@ -199,6 +205,37 @@ def test_many_sequences(fem):
     c.check(c.read())
 
 
+@pytest.mark.parametrize("causal", [True, False])
+def test_many_sequences_of_all_sizes(fem, causal):
+    """More sequences than lanes, chunks and single tokens mixed."""
+    say("many sequences of all sizes", causal)
+    rng = np.random.default_rng(4)
+    lens = [int(x) for x in rng.integers(1, 900, 90)]
+    news = [int(min(n, rng.choice([0, 1, 1, 1, 33, 150]))) for n in lens]
+    c = Call(fem, news, lens, 2, 1, 64, 64, 16, "int8", causal=causal, seed=4, tail=3)
+    out = c.read()
+    c.check(out)
+    assert torch.equal(out[:-3], c.read(cache=c.same)[:-3])
+
+
+@pytest.mark.parametrize("kv", list(DT))
+def test_chunks_and_tokens_with_long_contexts(fem, kv):
+    """Both kinds of rows split over their keys in one call."""
+    say("chunks and tokens", kv)
+    c = Call(fem, [1, 70, 1, 300, 2], [9000, 5000, 1, 6100, 3000], 2, 2, 64, 64, 64, kv, seed=6)
+    c.check(c.read())
+
+
+def test_shared_pages(fem):
+    """Two sequences whose first pages are the same ones."""
+    say("shared pages")
+    for n in (1, 50):
+        c = Call(fem, [n, n], [320, 320], 2, 1, 64, 64, 64, seed=n)
+        c.table[1, :4] = c.table[0, :4]
+        c.batch.table.copy_(torch.from_numpy(c.table))
+        c.check(c.read())
+
+
 @pytest.mark.parametrize("beta", [(1e-3, 1e-3), (0.499, 0.501), (16.0, 64.0)])
 def test_temperatures(fem, beta):
     say("beta", beta)
@@ -206,12 +243,13 @@ def test_temperatures(fem, beta):
     c.check(c.read())
 
 
+@pytest.mark.parametrize("d,dv", [(64, 64), (128, 128), (32, 32)])
 @pytest.mark.parametrize("news", [[1, 2], [140, 300]])
-def test_wide_ranges(fem, news):
+def test_wide_ranges(fem, news, d, dv):
     """Scores spread over hundreds of octaves and values too: sums that fall out of
     the kernels' common frames are formed again."""
-    say("wide ranges", news)
-    c = Call(fem, news, [700, 300], 1, 1, 64, 64, 64, qs=40.0, vs=12.0, beta=(1.0, 16.0), seed=11)
+    say("wide ranges", news, d, dv)
+    c = Call(fem, news, [700, 300], 1, 1, d, dv, 64, qs=40.0, vs=12.0, beta=(1.0, 16.0), seed=11)
     c.check(c.read())
 
 

@@ -74,7 +74,7 @@ def test_batch_is_checked(lib, call):
     for name in ("n_seq", "table_len"):
         assert call(lib, s=batch(**{name: 0})) == SHAPE, name
     assert call(lib, s=batch(n_seq=65536)) == SHAPE
-    assert call(lib, s=batch(table_len=(1 << 26) + 1)) == SHAPE  # more than 2^30 tokens
+    assert call(lib, s=batch(table_len=(1 << 22) + 1)) == SHAPE  # more than 2^26 tokens
     if call is not gather:
         assert call(lib, s=batch(q_start=None)) == NULLPTR
         for name in ("n_tok", "max_q"):
@@ -123,6 +123,11 @@ def test_read_arguments(lib):
     assert fwd(lib, c) == WORKSPACE
     assert fwd(lib, c, ws=A, n=need - 1) == WORKSPACE
     assert fwd(lib, c, ws=A + 16, n=need) == ALIGN
+
+
+def test_too_many_workgroups(lib):
+    c, s = cache(heads=65535, pages=1), batch(n_seq=65535, n_tok=1 << 14, max_q=1 << 14)
+    assert fwd(lib, c, s, H=65535, ld=65535 * 64, ws=A, n=1 << 60) == SHAPE
 
 
 def test_workspace_is_a_function_of_the_sizes(lib):
