@@ -20,6 +20,9 @@
  *
  * and the two-level gated read of the paper's models, which mixes F at a
  * per-channel beta_max with the prior's expectation (fem_softmax_gated_fwd).
+ * For serving: one token against a dense cache (fem_softmax_decode), and a paged,
+ * optionally quantised cache with the read of any number of new tokens over it
+ * (fem_cache_append, fem_cache_gather, fem_paged_fwd).
  *
  * Conventions shared by every entry point:
  *   - Every tensor argument is a DEVICE pointer (HIP device memory, e.g.

@@ -10,7 +10,8 @@ namespace fem {
 namespace {
 constexpr int kUnits = 256;      // compute units
 // Contexts that are not split: eight waves have four tiles each at most, which
-// takes about as long as the merge of splits would (B1 H8 L701 d64: KSHORT).
+// takes about as long as the merge of splits would (one token, 8 heads,
+// 701 keys, d = 64: 12.5 us, and 14.4 with four waves, splits and a merge).
 constexpr int kShortKeys = 1024;
 constexpr int kMergeRows = 8;    // of a merge's workgroup, few rows a block
 
