@@ -379,9 +379,9 @@ typedef enum {
  * an inf or NaN gets the byte 255 and reads as NaN.
  */
 typedef struct {
-  void* k;                /* 16-byte aligned                                   */
+  void* k;                /* all four 16-byte aligned                          */
   void* v;
-  unsigned char* k_scale; /* NULL for FEM_KV_BF16                              */
+  unsigned char* k_scale; /* not used with FEM_KV_BF16                         */
   unsigned char* v_scale;
   int pages;              /* >= 1                                              */
   int page;               /* tokens of a page: a power of two, 16 .. 1024      */

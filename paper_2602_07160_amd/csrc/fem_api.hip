@@ -70,6 +70,8 @@ int paged_args(const fem_paged_cache* c, const fem_paged_batch* s, bool tokens, 
       (unsigned long long)s->table_len * c->page > (1ull << 26))
     return FEM_ERR_SHAPE;
   if (!aligned16(c->k) || !aligned16(c->v)) return FEM_ERR_ALIGN;
+  if (c->type != FEM_KV_BF16 && (!aligned16(c->k_scale) || !aligned16(c->v_scale)))
+    return FEM_ERR_ALIGN;
   a->k = static_cast<const uint8_t*>(c->k);
   a->v = static_cast<const uint8_t*>(c->v);
   a->ks = c->k_scale;

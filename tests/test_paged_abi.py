@@ -65,6 +65,8 @@ def test_cache_is_checked(lib, call):
     assert call(lib, cache(pages=1 << 30, heads=1 << 10)) == SHAPE
     assert call(lib, cache(k=A + 8)) == ALIGN
     assert call(lib, cache(v=A + 4)) == ALIGN
+    assert call(lib, cache(k_scale=A + 4)) == ALIGN
+    assert call(lib, cache(v_scale=A + 8)) == ALIGN
 
 
 @pytest.mark.parametrize("call", CALLS)
