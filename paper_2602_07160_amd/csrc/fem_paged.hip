@@ -97,7 +97,7 @@ hipError_t launch_paged_read(const PagedArgs& a, const PagedPlan& plan, int kv, 
   MergePart few = {}, many = {};
   auto part = [&](MergePart& m, const Work& w, const int* tps, const float* at, int rps,
                   size_t blocks, int rows) {
-    m = MergePart{w, tps, at, rps, rows, 0};
+    m = MergePart{w, tps, at, rps, rows, 0, kLog2e / sqrtf((float)dk)};
     m.groups = (int)(blocks * ((rps + m.rows - 1) / m.rows));
   };
   if (plan.rows && plan.target)

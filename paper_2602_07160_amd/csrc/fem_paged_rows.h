@@ -24,8 +24,12 @@
 //   * The next tile's K and V are loaded into the registers that this tile's
 //     products and LDS writes have just freed, so a whole tilt hides them.
 //
-// What bounds it: HBM (a tile of 32 keys at d = 128 moves 16 KiB for ~2700
-// vector cycles of tilt on one of a compute unit's four SIMDs).
+// What bounds it: HBM where there are enough keys.  8 x 16 heads of up to 4096 keys
+// of d = 128 in bf16: 41.5 us, 4.65 TB/s of the 4.94 that a copy reaches; 16 x 8 heads
+// of up to 32768 keys in e4m3, four query heads each: 160 us, 4.5 TB/s (672 vector
+// instructions a tile, the vector units busy for 106 us of it).  Short splits are
+// bound by a workgroup's start and end, int8 by its conversion too (13 sequences of
+// 16 rows, d = 64: 30 us for 13 of bytes).
 //
 // Range.  P and E carry a bias of 40 and a lag of 8 each: their product is at
 // most 2^96, and a term that underflows in either factor is at most 2^-70 of
@@ -53,7 +57,7 @@ constexpr int kRowWaves = 4;       // of a workgroup; calls with short contexts 
                                    // many and do not split (kShortKeys)
 constexpr float kRowBias = 40.f;   // of P and of E
 constexpr float kLag = 8.f;        // of m and of c
-constexpr float kNone = -1e30f;    // m and c before the first key: finite, so that a hidden
+constexpr float kNone = -3e38f;    // m and c before the first key: finite, so that a hidden
                                    // key's exponent is -inf and not NaN
 constexpr float kLoBelow = 0.5f;   // channels with beta below this take E as hi + lo
 
@@ -266,11 +270,11 @@ __device__ __forceinline__ int row_limit(const Seq& s, int r, int G, bool causal
 
 // ---- exact form ---------------------------------------------------------------
 
-// log2 sum over keys [k0, k1) of 2^(s_i + bl v_ij), formed by a whole wave in
-// fp32; returns -inf for no keys.
+// log2 sum over keys [k0, k1) of 2^((s_i - ref) scale2 + bl v_ij), formed by a whole
+// wave in fp32; returns -inf for no keys.
 template <int DK, int DV, int KV>
 __device__ float exact_joint(const PagedArgs& a, const bf16* qrow, int b, int g, int j, float bl,
-                             int k0, int k1, float scale2) {
+                             int k0, int k1, float scale2, float ref) {
   Lse2 t;
   for (int i = k0 + (threadIdx.x & 63); i < k1; i += 64) {
     bool bad = false;
@@ -288,7 +292,7 @@ __device__ float exact_joint(const PagedArgs& a, const bf16* qrow, int b, int g,
     row8<KV, DV>(a.v, a.vs, row, j >> 3, f);
 #pragma unroll
     for (int e = 0; e < 8; ++e) v = (j & 7) == e ? f[e] : v;
-    t.add(fmaf(v, bl, dot * scale2));
+    t.add(fmaf(v, bl, (dot - ref) * scale2));
   }
   return t.wave_total();
 }
@@ -338,7 +342,7 @@ struct RowRead {
 
   bf16x8 qf[RB][C::NKS];
   f32x4 acc[RB][C::NCB];
-  float m[RB];
+  float m[RB];     // of the scores before scale2
   f32x4 lsum[RB];  // sums of rows 4 grp + i, the same in every lane of the group
   float bl[C::NCB], c[C::NCB];
   unsigned lo_blocks;  // bit cb: a channel of the block takes hi + lo
@@ -485,10 +489,11 @@ struct RowRead {
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
       float x[8];
+      // m is subtracted from the scores as they are: a product rounded otherwise than
+      // m's own would leave the largest score off by half its last place
       auto exponents = [&] {
-        const float sh = kRowBias - m[rb];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = fmaf(s[rb][e >> 2][e & 3], scale2, sh);
+        for (int e = 0; e < 8; ++e) x[e] = fmaf(s[rb][e >> 2][e & 3] - m[rb], scale2, kRowBias);
         return max8(x);
       };
       if (masked) {
@@ -500,9 +505,9 @@ struct RowRead {
       if (__any(exponents() > kRowBias + kLag)) {
         float mx = fmaxf(fmaxf(fmaxf(s[rb][0][0], s[rb][0][1]), fmaxf(s[rb][0][2], s[rb][0][3])),
                          fmaxf(fmaxf(s[rb][1][0], s[rb][1][1]), fmaxf(s[rb][1][2], s[rb][1][3])));
-        mx = max_groups(mx) * scale2;
-        const float mn = mx > m[rb] + kLag ? mx : m[rb];
-        const float f = mn == m[rb] ? 1.f : exp2_hw(m[rb] - mn);
+        mx = max_groups(mx);
+        const float mn = (mx - m[rb]) * scale2 > kLag ? mx : m[rb];
+        const float f = mn == m[rb] ? 1.f : exp2_hw((m[rb] - mn) * scale2);
         m[rb] = mn;
         f32x4 fr;
 #pragma unroll
@@ -604,7 +609,7 @@ struct ReadArgs {
   const float* beta;   // [heads][DV]
   void* out;           // [ntok][H][DV] float32 or bf16
   int* tps;            // [2] tiles of a split, as the two kernels have chosen them
-  float* part;         // [slot][rps][part_row]: log2 joint sums, the row's log2 normaliser
+  float* part;         // [slot][rps][part_row]
   float* wide_part;    // of the wide kernel
   int H, G;            // query heads, of a cached head
   int rps, wide_rps;   // rows of a slot
@@ -619,8 +624,10 @@ __host__ __device__ __forceinline__ Work rows_work(const PagedArgs& a, const Rea
   return Work{r.G, kRowsMax, kRowTile, 0, r.most_rows, a.max_q, r.causal != 0, false};
 }
 
-// A row of partial results: its channels' sums, its normaliser, and room to keep the
-// next row aligned for loads of four.
+// A row of partial results: log2 of its channels' joint sums and of its own sum, both
+// less the row's maximum in the range (which may be far larger than what they differ
+// by), that maximum in the scores' own scale, and room to keep the next row aligned for
+// loads of four.
 __host__ __device__ constexpr int part_row(int dv) { return dv + 4; }
 
 __device__ __forceinline__ void put4(const ReadArgs& r, size_t at, f32x4 x) {
@@ -736,7 +743,7 @@ __device__ __forceinline__ void rows_body(const PagedArgs& a, const ReadArgs& r,
     const float M = top_of(fm + tid, kRowsMax);
     float l = 0.f;
 #pragma unroll
-    for (int x = 0; x < NW; ++x) l += fl[x * kRowsMax + tid] * exp2_hw(fm[x * kRowsMax + tid] - M);
+    for (int x = 0; x < NW; ++x) l += fl[x * kRowsMax + tid] * exp2_hw((fm[x * kRowsMax + tid] - M) * scale2);
     rm[tid] = M;
     rl[tid] = l;
   }
@@ -754,7 +761,7 @@ __device__ __forceinline__ void rows_body(const PagedArgs& a, const ReadArgs& r,
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int q = rb * 16 + 4 * w.grp + i;
-      rf[i] = exp2_hw(fm[wave * kRowsMax + q] - top_of(fm + q, kRowsMax));
+      rf[i] = exp2_hw((fm[wave * kRowsMax + q] - top_of(fm + q, kRowsMax)) * scale2);
     }
     float* area = reinterpret_cast<float*>(smem + wave * C::AREA);
 #pragma unroll
@@ -777,8 +784,9 @@ __device__ __forceinline__ void rows_body(const PagedArgs& a, const ReadArgs& r,
       const float blj = r.beta[g * DV + j] * kLog2e;
       const int seen = min(kend, row_limit(sq, row, r.G, causal));  // of this range, up to here
       const bool none = !live || seen <= kbeg;
-      float y = none ? -INFINITY : log2_hw(sum) + (M + top - 2.f * kRowBias);
-      const float lp = none ? -INFINITY : log2_hw(l) + (M - kRowBias);
+      // logarithms of the joint sum and of the row's sum, both less M
+      float y = none ? -INFINITY : log2_hw(sum) + (top - 2.f * kRowBias);
+      const float lp = none ? -INFINITY : log2_hw(l) - kRowBias;
       bool redo = !none && !bad && !(sum >= 0x1p-40f);
       uint64_t who = __ballot(redo);
       while (who != 0) {
@@ -788,8 +796,10 @@ __device__ __forceinline__ void rows_body(const PagedArgs& a, const ReadArgs& r,
         const int ee = __builtin_amdgcn_readlane(seen, src);
         const bf16* qp = r.q + (size_t)(sq.q0 + rr / r.G) * (size_t)r.qld +
                          (size_t)(g * r.G + rr % r.G) * DK;
+        const float ref = __uint_as_float(
+            (unsigned)__builtin_amdgcn_readlane((int)__float_as_uint(M), src));
         const float x = exact_joint<DK, DV, KV>(a, qp, it.b, g, jj, r.beta[g * DV + jj] * kLog2e,
-                                                kbeg, ee, scale2);
+                                                kbeg, ee, scale2, ref);
         if (w.lane == src) y = x;
       }
       if (!live) continue;
@@ -802,7 +812,10 @@ __device__ __forceinline__ void rows_body(const PagedArgs& a, const ReadArgs& r,
       } else {
         float* p = r.part + ((size_t)slot * r.rps + rb * 16 + q) * part_row(DV);
         p[j] = bad ? NAN : y;
-        if (j == 0) p[DV] = bad ? NAN : lp;
+        if (j == 0) {
+          p[DV] = bad ? NAN : lp;
+          p[DV + 1] = none ? -INFINITY : M;
+        }
       }
     }
   }
@@ -872,11 +885,13 @@ struct MergePart {
   const int* tps;
   const float* part;
   int rps, rows, groups;  // rows of a slot, of a chunk; workgroups
+  float scale2;           // of the scores
 };
 
 constexpr int kMergeThreads = 256;
 constexpr int kMergeBatch = 8;
 
+// Bound by latency: about 5.5 us for 13 x 8 heads of 16 rows in five splits.
 // Workgroup (chunk of a row block, cached head); the first p.groups of them for p,
 // the others for o.  A thread has four channels of a row; a row's splits are shared
 // by so many threads (a power of two) that each takes one batch of them, if there
@@ -886,7 +901,7 @@ __global__ __launch_bounds__(kMergeThreads) void paged_merge_kernel(PagedArgs a,
                                                                     MergePart p, MergePart o) {
   constexpr int TPR = DV / 4, NG = kMergeThreads / TPR;  // threads of a row, groups of them
   __shared__ f32x4 meet_m[NG][TPR], meet_s[NG][TPR];
-  __shared__ float meet_d[NG][2];
+  __shared__ float meet_d[NG][3];
   __shared__ int item[kItemInts];
   const bool second = (int)blockIdx.x >= p.groups;
   const MergePart& x = second ? o : p;
@@ -906,49 +921,62 @@ __global__ __launch_bounds__(kMergeThreads) void paged_merge_kernel(PagedArgs a,
   int per = 1;  // groups of a row
   while (per < NG && per * kMergeBatch < it.ns) per <<= 1;
   const int rows = NG / per, grp = threadIdx.x / TPR, c = threadIdx.x % TPR, sub = grp % per;
-  const f32x4 bl = *reinterpret_cast<const f32x4*>(r.beta + g * DV + c * 4) * kLog2e;
+  f32x4 bl;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) bl[e] = r.beta[g * DV + c * 4 + e] * kLog2e;
   constexpr int PR = part_row(DV);
   const size_t step = (size_t)a.heads * x.rps * PR;  // from split to split
   const float* base = x.part + ((size_t)((size_t)it.slot * a.heads + g) * x.rps + c0) * PR;
   const f32x4 kNone4 = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
   for (int q0 = 0; q0 < nr; q0 += rows) {
     const int q = q0 + grp / per;
+    // sums as (max, sum) of 2^x, x less the largest row maximum so far, ref
     f32x4 M = kNone4, S = {0.f, 0.f, 0.f, 0.f};
-    float md = -INFINITY, sd = 0.f;
+    float md = -INFINITY, sd = 0.f, ref = kNone;
     if (q < nr) {
       const float* pq = base + (size_t)q * PR;
       for (int s0 = sub; s0 < it.ns; s0 += kMergeBatch * per) {
         f32x4 y[kMergeBatch];
-        float d[kMergeBatch];
+        float d[kMergeBatch], m[kMergeBatch];
 #pragma unroll
         for (int u = 0; u < kMergeBatch; ++u) {
           const int s = s0 + u * per;
           const float* ps = pq + step * min(s, it.ns - 1);
           y[u] = *reinterpret_cast<const f32x4*>(ps + c * 4);
           d[u] = ps[DV];
+          m[u] = ps[DV + 1];
           if (s >= it.ns) {
             y[u] = kNone4;
             d[u] = -INFINITY;
+            m[u] = -INFINITY;
           }
         }
+        float now = ref;
+#pragma unroll
+        for (int u = 0; u < kMergeBatch; ++u) now = fmaxf(now, m[u]);
+#pragma unroll
+        for (int u = 0; u < kMergeBatch; ++u) m[u] = (m[u] - now) * x.scale2;
+        const float old = (ref - now) * x.scale2;
+        ref = now;
         // the batch's maximum first: its exponentials then wait for nothing else
-        auto fold = [&](float& m, float& z, auto&& at) {
+        auto fold = [&](float& mm, float& z, auto&& at) {
           float top = at(0), sum = 0.f;
 #pragma unroll
           for (int u = 1; u < kMergeBatch; ++u) top = fmaxf(top, at(u));
-          const float ref = fmaxf(top, -3e38f);  // none of the batch: zeros, or NaN
+          const float zero = fmaxf(top, -3e38f);  // none of the batch: zeros, or NaN
 #pragma unroll
-          for (int u = 0; u < kMergeBatch; ++u) sum += exp2_hw(at(u) - ref);
-          lse_join(m, z, top, sum);
+          for (int u = 0; u < kMergeBatch; ++u) sum += exp2_hw(at(u) - zero);
+          mm += old;
+          lse_join(mm, z, top, sum);
         };
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          float m = M[e], z = S[e];
-          fold(m, z, [&](int u) { return y[u][e]; });
-          M[e] = m;
+          float mm = M[e], z = S[e];
+          fold(mm, z, [&](int u) { return y[u][e] + m[u]; });
+          M[e] = mm;
           S[e] = z;
         }
-        fold(md, sd, [&](int u) { return d[u]; });
+        fold(md, sd, [&](int u) { return d[u] + m[u]; });
       }
     }
     const int row = r0 + q;
@@ -966,17 +994,21 @@ __global__ __launch_bounds__(kMergeThreads) void paged_merge_kernel(PagedArgs a,
     if (c == 0) {
       meet_d[grp][0] = md;
       meet_d[grp][1] = sd;
+      meet_d[grp][2] = ref;
     }
     __syncthreads();
     if (q >= nr) continue;
     // the row's groups share its channels
     const int g0 = grp - sub;
+    float top = meet_d[g0][2];
+    for (int u = 1; u < per; ++u) top = fmaxf(top, meet_d[g0 + u][2]);
     auto join = [&](auto&& max_of, auto&& sum_of, float& m, float& z) {
-      m = max_of(0);
-      for (int u = 1; u < per; ++u) m = fmaxf(m, max_of(u));
-      const float ref = fmaxf(m, -3e38f);
+      auto at_top = [&](int u) { return max_of(u) + (meet_d[g0 + u][2] - top) * x.scale2; };
+      m = at_top(0);
+      for (int u = 1; u < per; ++u) m = fmaxf(m, at_top(u));
+      const float zero = fmaxf(m, -3e38f);
       z = 0.f;
-      for (int u = 0; u < per; ++u) z += sum_of(u) * exp2_hw(max_of(u) - ref);
+      for (int u = 0; u < per; ++u) z += sum_of(u) * exp2_hw(at_top(u) - zero);
     };
     join([&](int u) { return meet_d[g0 + u][0]; }, [&](int u) { return meet_d[g0 + u][1]; }, md, sd);
     for (int e = sub; e < 4; e += per) {

@@ -21,7 +21,8 @@
 //     underflows is at most 2^-46 of the frame; a sum below 2^-20 is formed again,
 //     exactly.
 //
-// MFMA-bound, like the dense read.
+// MFMA-bound, like the dense read: 4096 tokens behind 12288, 16 heads of 128 in bf16,
+// 650 us, 740 TFLOP/s.
 #pragma once
 
 #include "fem_paged_rows.h"
@@ -33,7 +34,7 @@ namespace {
 constexpr int kWideRows = 256;
 constexpr int kWideTile = 64;
 constexpr float kWideLow = 0x1p-20f;
-constexpr float kNoMax = -1e30f;  // row maximum before the first visible key
+constexpr float kNoMax = -3e38f;  // row maximum before the first visible key
 
 template <class C, int KV>
 struct WideLds {
@@ -58,6 +59,39 @@ struct PairSlots {
   __device__ static __forceinline__ unsigned offset(int s) {
     const int row = s / SPR, chunk = s % SPR;
     return (unsigned)(row * W + (chunk < W / 8 ? chunk * 8 : 0)) * 2u;
+  }
+};
+
+// The softmax of a paged read keeps its maximum m in the scores' own scale.  One fma a
+// score, s scale2 - m scale2, is off by half the last place of m scale2: 2^-15 at 2^10,
+// more than a 2^x can hold from 2^30 on.  A tile with such a row has m subtracted first.
+// (It costs 1 %: 4096 rows over 16384 keys took 702 us for 695.  Subtracted always, two
+// operations a score, it was 2.8 %.)
+template <int NKB>
+struct WideSoftmax : Softmax<NKB> {
+  float mm;  // what the fma subtracts
+  __device__ __forceinline__ void update(float& m, float& apend, float scale2) {
+    const float x = fmaxf(this->mx, other_half(this->mx));
+    const float mnew = (x - m) * scale2 > kRowLag ? x : m;
+    apend = mnew == m ? 1.f : exp2_hw((m - mnew) * scale2);
+    m = mnew;
+  }
+  __device__ __forceinline__ void shift(f32x16 (&sc)[NKB], float m, float scale2) {
+    const float ms = fmaxf(m, -3e38f);  // (no key yet: every score is -inf)
+    mm = ms * scale2;
+    if (__any(fabsf(mm) > 0x1p10f)) {
+#pragma unroll
+      for (int kb = 0; kb < NKB; ++kb)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sc[kb][i] -= ms;
+      mm = 0.f;
+    }
+  }
+  __device__ __forceinline__ void prob_arg(const f32x16 (&sc)[NKB], f32x2& x, int q, float,
+                                           float scale2) const {
+    const int ks = q >> 2, u = 2 * (q & 3), kb = ks >> 1, s0 = (ks & 1) * 8;
+    x[0] = fmaf(sc[kb][s0 + u], scale2, -mm);
+    x[1] = fmaf(sc[kb][s0 + u + 1], scale2, -mm);
   }
 };
 
@@ -304,7 +338,7 @@ __device__ __forceinline__ void wide_body(const PagedArgs& a, const ReadArgs& r,
   phase1<C, NLO, PVA, QKT>(sm, tl, k, n_eff - (tb + k) * kWideTile, wave, lane, kofs, eofs, vcol, qf, \
                            sacc, acc, lacc, PPREV, lsel, SIDE)
 #define FEM_WIDE2(PVB, SM, MK, PPREV, PNEXT)                                                  \
-  phase2<C, NLO, PVB, SM, MK>(sm, acc, PPREV, PNEXT, sacc, m, apend, k - 1, eofs,             \
+  phase2<C, NLO, PVB, SM, MK, WideSoftmax<C::NKB>>(sm, acc, PPREV, PNEXT, sacc, m, apend, k - 1, eofs,             \
                               (tb + k) * kWideTile + kg * 32, tm, hl, scale2)
   const auto none = [](auto...) __attribute__((always_inline)) {};
   {
@@ -366,7 +400,8 @@ __device__ __forceinline__ void wide_body(const PagedArgs& a, const ReadArgs& r,
     __syncthreads();
     if (kg == 1) return;
     const float m1 = stage[NX * 64 + lane], l1 = stage[(NX + 1) * 64 + lane];
-    const float mm = fmaxf(m, m1), f0 = exp2_hw(m - mm), f1 = exp2_hw(m1 - mm);
+    const float mm = fmaxf(m, m1);
+    const float f0 = exp2_hw((m - mm) * scale2), f1 = exp2_hw((m1 - mm) * scale2);
 #pragma unroll
     for (int cb = 0; cb < C::NCB; ++cb)
 #pragma unroll
@@ -381,7 +416,7 @@ __device__ __forceinline__ void wide_body(const PagedArgs& a, const ReadArgs& r,
   const int seen = min(kend, tm + 1);  // end of this row's keys in the range
   const bool empty = seen <= kbeg, single = it.ns == 1;
   const float lt = lacc[0], rl = 0x1p-64f / lt;
-  const float lp = empty ? -INFINITY : m + log2_hw(lt);
+  const float lp = empty ? -INFINITY : log2_hw(lt);  // (less m, as the channels' sums)
   const float* cw = sm.c((ntiles - 1) & 1);
   const float* inv = sm.inv();
   const auto low = [&](float x) { return !(x >= kWideLow && x * rl >= 0x1p-120f); };
@@ -401,7 +436,7 @@ __device__ __forceinline__ void wide_body(const PagedArgs& a, const ReadArgs& r,
           if (low(acc[cb][i]) && mine && !empty && !bad) flags |= 1ull << (cb * 16 + i);
     }
   }
-  // one split: F; else log2 of the joint sum, (log2 acc - bias + c) + m
+  // one split: F; else log2 of the joint sum less m, log2 acc - bias + c
 #pragma unroll
   for (int cb = 0; cb < C::NCB; ++cb) {
 #pragma unroll
@@ -413,7 +448,7 @@ __device__ __forceinline__ void wide_body(const PagedArgs& a, const ReadArgs& r,
       for (int e = 0; e < 4; ++e) {
         const float x = acc[cb][q * 4 + e];
         float o = single ? (log2_hw(x * rl) + cw[ch0 + e]) * inv[ch0 + e]
-                         : log2_hw(x * rl) + log2_hw(lt) + (cw[ch0 + e] + m);
+                         : log2_hw(x * rl) + log2_hw(lt) + cw[ch0 + e];
         if (empty) o = -INFINITY;  // (never with one split)
         stage[n * SROW + oc[e]] = bad ? __builtin_nanf("") : o;
       }
@@ -428,8 +463,10 @@ __device__ __forceinline__ void wide_body(const PagedArgs& a, const ReadArgs& r,
         (uint64_t)(unsigned)__builtin_amdgcn_readlane((int)(unsigned)(flags >> 32), src) << 32 |
         (unsigned)__builtin_amdgcn_readlane((int)(unsigned)flags, src);
     const int rr = __builtin_amdgcn_readlane(row, src), ee = __builtin_amdgcn_readlane(seen, src);
-    const float dl = __uint_as_float(
-        (unsigned)__builtin_amdgcn_readlane((int)__float_as_uint(lp), src));
+    auto lane_of = [src](float x) {
+      return __uint_as_float((unsigned)__builtin_amdgcn_readlane((int)__float_as_uint(x), src));
+    };
+    const float dl = lane_of(lp), ref = lane_of(m);
     const bf16* qp = r.q + (size_t)(sq.q0 + rr / r.G) * (size_t)r.qld +
                      (size_t)(g * r.G + rr % r.G) * C::DK;
     for (uint64_t f = fw; f != 0; f &= f - 1) {
@@ -437,7 +474,7 @@ __device__ __forceinline__ void wide_body(const PagedArgs& a, const ReadArgs& r,
       const int col = cb * 32 + (i >> 2) * 8 + (src >> 5) * 4 + (i & 3);
       const int j = SPLIT ? sm.chan()[col] : col;
       const float bl = sm.bl()[col];
-      const float y = exact_joint<C::DK, C::DV, KV>(a, qp, it.b, g, j, bl, kbeg, ee, scale2);
+      const float y = exact_joint<C::DK, C::DV, KV>(a, qp, it.b, g, j, bl, kbeg, ee, scale2, ref);
       if (lane == 0) stage[(src & 31) * SROW + j] = single ? (y - dl) / bl : y;
     }
   }
@@ -447,7 +484,10 @@ __device__ __forceinline__ void wide_body(const PagedArgs& a, const ReadArgs& r,
   if (!single) {
     constexpr int PR = part_row(C::DV);
     float* p = r.wide_part + ((size_t)slot_id * r.wide_rps + wr0) * PR;
-    if (hl == 0 && mine) p[n * PR + C::DV] = bad ? __builtin_nanf("") : lp;
+    if (hl == 0 && mine) {
+      p[n * PR + C::DV] = bad ? __builtin_nanf("") : lp;
+      p[n * PR + C::DV + 1] = empty ? -INFINITY : m;
+    }
 #pragma unroll 4
     for (int q = 0; q < 32; q += RPI) {
       const int rr = q + lane / LPR;

@@ -442,6 +442,7 @@ struct Softmax {
     apend = (mnew == m) ? 1.f : exp2_hw(m - mnew);
     m = mnew;
   }
+  __device__ __forceinline__ void shift(f32x16 (&)[NKB], float, float) {}
   // The probabilities of pair q (k-step q / 4, entries 2 (q % 4), +1) in three
   // stages, placed one slot apart so that no stage waits on the one before:
   // the exponents, 2^exponent, and the rounding into the MFMA B operand.
@@ -591,7 +592,7 @@ __device__ __forceinline__ void phase1(const Smem<C>& sm, Tilt<C>& tl, int k, in
 // from pp, interleaved by hand with the softmax of this tile (SM; MASK on the
 // wave's diagonal tile and the tiles after it), which writes P(k) into the
 // other buffer pn.  The softmax's stages sit one slot apart as in phase 1.
-template <class C, int NLO, bool PVB, bool SM, bool MASK>
+template <class C, int NLO, bool PVB, bool SM, bool MASK, class Smx = Softmax<C::NKB>>
 __device__ __forceinline__ void phase2(const Smem<C>& sm, f32x16 (&acc)[C::NCB],
                                        const bf16x8 (&pp)[C::KS], bf16x8 (&pn)[C::KS],
                                        f32x16 (&sc)[C::NKB],
@@ -619,7 +620,6 @@ __device__ __forceinline__ void phase2(const Smem<C>& sm, f32x16 (&acc)[C::NCB],
 #pragma unroll
   for (int f = 0; f < RING; ++f)
     if (f < NF) ring[f] = frag(f);
-  using Smx = Softmax<C::NKB>;
   Smx smx;
   f32x2 px[NP];
   if (SM) smx.template mask<MASK>(sc, k0, tq, hl);
@@ -636,9 +636,12 @@ __device__ __forceinline__ void phase2(const Smem<C>& sm, f32x16 (&acc)[C::NCB],
       if (st == 0) smx.max1(sc, 0);
       if (st == 1) smx.max1(sc, 1);
       if (st == 2) smx.max2();
-      if (st == 3) smx.update(m, apend, scale2);
+      if (st == 3) {
+        smx.update(m, apend, scale2);
+        smx.shift(sc, m, scale2);
+      }
       const int qa = st - P0, qe = qa - 1, qr = qa - 2;  // pairs at each stage
-      if (qa >= 0 && qa < NP) Smx::prob_arg(sc, px[qa], qa, m, scale2);
+      if (qa >= 0 && qa < NP) smx.prob_arg(sc, px[qa], qa, m, scale2);
       if (qe >= 0 && qe < NP) Smx::prob_exp(px[qe]);
       if (qr >= 0 && qr < NP) Smx::template prob_round<C::KS>(px[qr], pn, qr);
     }

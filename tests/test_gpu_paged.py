@@ -267,6 +267,43 @@ def test_opposed_ranges(fem, n):
     c.check(c.read())
 
 
+@pytest.mark.parametrize("n", [1, 3, 60, 200])
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+def test_scores_of_any_size(fem, n, sign):
+    """Scores near the ends of float32, all of one sign: one key has all the weight."""
+    say("huge scores", n, sign)
+    c = Call(fem, [n], [n + 300], 1, 2, 64, 64, 64, seed=13, stale=0.0)
+    c.cache.k.abs_().mul_(sign * 1e15)
+    c.q.abs_().mul_(1e20)
+    c.check(c.read())
+
+
+@pytest.mark.parametrize("kv", ["bf16", "int8"])
+@pytest.mark.parametrize("news,lens", [([1], [9000]), ([3, 1], [700, 5000]), ([40], [3000]), ([70], [70])])
+def test_large_scores_that_differ_little(fem, news, lens, kv):
+    """Every score is 126976 and a small part, exactly; only the small parts count."""
+    say("offset scores", news, lens, kv)
+    c = Call(fem, news, lens, 1, 4, 64, 64, 64, kv=kv, seed=14, stale=0.0)
+    c.q[:] = 64.0
+    c.q[..., 1], c.q[..., 32:] = 0.125, 0.0  # 31 x 64 x 512 / sqrt(64), and j / 8
+    rows = getattr(c, "same", c.cache).k
+    j = torch.arange(rows.shape[0] * rows.shape[2], device="cuda").view(-1, 1, rows.shape[2]) * 7 % 33
+    rows[:], rows[..., 1] = 512.0, (8 * j).bfloat16()
+    if kv != "bf16":
+        c.cache.k[:], c.cache.k[..., 1] = 64, j.to(torch.int8)
+        c.cache.k_scale[:] = 127 + 3
+    c.check(c.read())
+
+
+def test_beta_anywhere(fem):
+    """beta needs no alignment of its own."""
+    say("beta")
+    c = Call(fem, [1, 40], [3000, 500], 2, 1, 64, 64, 64)
+    want = c.read()
+    c.beta = torch.cat((c.beta.new_zeros(1), c.beta.flatten()))[1:].view(2, 64)
+    assert c.beta.data_ptr() % 16 and torch.equal(c.read(), want)
+
+
 def test_outputs_and_padding(fem):
     """bf16 output; rows behind the last sequence and sequences without tokens."""
     say("outputs")
