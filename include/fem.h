@@ -374,7 +374,8 @@ typedef enum {
  * stored as the byte e + 127 in k_scale [pages, heads, page, d_qk / 32] and
  * v_scale [.., d_v / 32].  e is the smallest integer, at least -100, with
  * max |x| <= M 2^e, M = 448 (e4m3) or 127 (int8); a code is x 2^-e rounded to
- * nearest even, so none saturates.  The value code 2^e is exactly a bf16 number:
+ * nearest even, so none saturates.  The value code 2^e is exactly a bf16 number
+ * (an infinity where the rounding passes the largest one, from 1.9375 2^127 on):
  * a read over a quantised cache is the bf16 read over its values.  A block with
  * an inf or NaN gets the byte 255 and reads as NaN.
  */
@@ -458,7 +459,8 @@ int fem_cache_gather(const fem_paged_cache* cache, const fem_paged_batch* batch,
  *           0 with FEM_FLAG_ENCODER) reads NaN.
  *   flags : an OR of fem_flags
  *
- * Cached rows at or past lens[b] may hold anything.  The same inputs give the same
+ * Cached rows at or past lens[b] may hold anything; an inf or NaN before it may
+ * reach every token of its sequence (and of no other).  The same inputs give the same
  * bits.  Probabilities enter the product as bf16, exponentials of channels with
  * beta < 0.5 as bf16 hi + lo parts, of the others as bf16 (2^-8 / beta of the
  * read at most); sums are float32.

@@ -515,7 +515,7 @@ class PagedBatch:
         self.n_tok = 0 if n_tok is None else int(n_tok)
         self.c = _Batch(None if q_start is None else q_start.data_ptr(), lens.data_ptr(),
                         table.data_ptr(), lens.shape[0], table.shape[1], self.n_tok,
-                        self.n_tok if max_q is None else int(max_q))
+                        self.n_tok if max_q is None else min(int(max_q), self.n_tok))
         self.ref = ctypes.byref(self.c)
 
 
