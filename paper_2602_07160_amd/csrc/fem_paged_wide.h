@@ -22,7 +22,7 @@
 //     exactly.
 //
 // MFMA-bound, like the dense read: 4096 tokens behind 12288, 16 heads of 128 in bf16,
-// 650 us, 740 TFLOP/s.
+// 685 us, 700 TFLOP/s.
 #pragma once
 
 #include "fem_paged_rows.h"
@@ -553,7 +553,7 @@ __device__ __forceinline__ int wide_tiles(const Planner& plan, const ReadArgs& r
 // that may have sequences of few rows too (r.rows_too), their splits follow, read as
 // paged_rows_kernel reads them but by eight waves: they fill the units that the last
 // wide items leave idle (twelve sequences of 1 to 700 tokens, of which two with one:
-// 496 us with a launch of their own, 471 so).
+// 496 us with a launch of their own, 471 so, then).
 template <int DK, int DV, int KV>
 __global__ __launch_bounds__(512) void paged_wide_kernel(PagedArgs a, ReadArgs r) {
   using C1 = Cfg<DK, DV, 8, kFem, true, false, 1>;
